@@ -307,6 +307,76 @@ uint64_t lsam_schedule_hash(uint64_t seed, int tag, uint64_t t, uint64_t k, uint
 int lsam_row_norms_static(const float* d_g, int64_t ld, int64_t n, int32_t K, float* d_norm, void* cuda_stream,
                           char* h_err, size_t h_err_len);
 
+/* ---- operators around a classifier's head ----
+ * For callers that run a model of their own beside this library (LSAM_MODEL_FLAT) and for scoring what a context has trained: the
+ * loss of a softmax head with its gradient, the scores of a head without its logits, and dropout that is the same in the two
+ * gradient passes of a tick.  (The paper has no counterpart; they follow the library's conventions.)
+ *  - No context, no allocation, no state between calls; everything is enqueued on cuda_stream (NULL = default stream) and may be
+ *    captured into a CUDA graph.  Calls on different streams are independent; what produced the inputs must be ordered before the call.
+ *  - d_* pointers are memory of the CURRENT device, aligned to their element type (checked: LSAM_ERR_INVALID, nothing is launched).
+ *  - Tensors of workers are stacked: index (k, row, column), strides in elements.  K = 1 for a single model.  Per-row arrays
+ *    (labels, logp, lse, ...) are dense [K, rows].  K = 0 or rows = 0 is a valid call that does nothing.
+ *  - Arithmetic in fp32 whatever the storage type; one rounding at the end where the result is stored in 16 bits.
+ *  - h_err: nullable host buffer of h_err_len bytes that receives a message when the call fails. */
+enum { LSAM_FP32 = 0, LSAM_BF16 = 1, LSAM_FP16 = 2 };
+
+/* Scores of rows of logits l[c], c < classes:
+ *   lse = log sum_c e^l[c];  logp = l[label] - lse;  entropy = -sum_c p_c log p_c, p_c = e^(l[c] - lse);
+ *   top_idx / top_logp [K, rows, top_k]: the top_k classes of largest logit in descending order, the lower class first among equals,
+ *   and their log probabilities.
+ *  d_logits   element (k, r, c) at k stride_k + r stride_row + c stride_class, strides >= 0; either stride may be the unit one (a
+ *             context's own logits have the sample index contiguous: stride_row = 1).
+ *  d_labels   nullable int32: a negative label leaves the row out (it is not read; logp = lse = entropy = 0, no alternatives); a
+ *             label >= classes makes logp NaN.
+ *  d_logp (needs d_labels), d_lse, d_entropy: nullable.  top_k = 0 .. LSAM_TOP_MAX; with 0 the two top arrays are not touched.
+ * Logits of -inf have probability 0 and are never alternatives: missing alternatives have index -1 and log probability -inf, a row with
+ * nothing but -inf has lse = -inf, logp = -inf, entropy 0.  A NaN or a +inf logit makes lse, entropy and every log probability of its row
+ * NaN (a label of logit -inf keeps -inf); NaN is never an alternative. */
+#define LSAM_TOP_MAX 32
+int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                 int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
+                 float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len);
+
+/* Gradient of a loss of logp and entropy with respect to the logits:
+ *   dlogits[c] = dlogp (1[c = label] - p_c) - dentropy p_c (log p_c + entropy),   p_c = e^(l[c] - lse)
+ * with lse and entropy [K, rows] as lsam_logprob returned them for the same logits, dlogp and dentropy [K, rows] the loss's derivatives
+ * (nullable: 0; not both NULL; dlogp needs d_labels, dentropy needs d_entropy).  The minibatch cross-entropy of a context is
+ * dlogp = -1 / batch.  Rows that are left out (negative label) and rows of nothing but
+ * masks (lse below -1e30: every logit -inf, or the lowest value of a type) get zeros; a label >= classes makes its row NaN.
+ * d_dlogits: type of the logits, strides of its own (no two elements at one address); may be d_logits itself with the same strides. */
+int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                      int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
+                      const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
+                      void* cuda_stream, char* h_err, size_t h_err_len);
+
+/* The first three results of lsam_logprob for the logits l = h w^T + bias, which are never stored:
+ *  d_h [K, rows, inner] and d_w [K, classes, inner] of `dtype`, the inner index contiguous; w_stride_k = 0 shares one head among the workers.
+ *  d_bias [K, classes] fp32 (bias_stride_k, 0 = shared) or NULL.  Labels and results as in lsam_logprob.
+ * Products are accumulated in fp32.  16-bit operands whose addresses and strides are multiples of 16 bytes run on the tensor cores.
+ *  d_workspace: lsam_head_logprob_workspace_bytes() bytes, 256-byte aligned, contents irrelevant before and after; calls that may overlap on
+ *  the GPU (other streams, graphs replayed side by side) need one each.
+ * K <= 65535, rows <= 4194240. */
+size_t lsam_head_logprob_workspace_bytes(int32_t K, int64_t rows, int64_t classes);
+int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
+                      int64_t h_stride_k, int64_t h_stride_row, int64_t w_stride_k, int64_t w_stride_class, int64_t bias_stride_k,
+                      const int32_t* d_labels, float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes,
+                      void* cuda_stream, char* h_err, size_t h_err_len);
+
+/* Dropout with a mask that is never stored:  out = skip + (kept ? x * scale : 0)  (skip NULL: 0), x, skip and out [K, rows, n] of `dtype`,
+ * columns contiguous.  Whether column c of row r of worker k_offset + k is kept is a function of (seed, tick, layer, worker, r, c) alone, so the ascent
+ * and the descent pass of a tick, and the backward pass of each, see the same mask: the backward pass is the same call on the gradient
+ * (d_skip = NULL; the gradient of skip is the output's).  Philox4x32-10 with
+ *   counter = (c / 8, r, layer 2^20 + worker, tick low 32 bits), key = (seed low ^ "drop", seed high ^ tick high)
+ * gives the 16-bit numbers of eight columns (word (c mod 8) / 2, low half first); a column is dropped when its number is below
+ * cut = floor(65536 p + 1/2), and scale = 65536 / (65536 - cut), so p is used to the nearest 2^-16 and the expectation is exact for it.
+ * Dropped elements are not multiplied: a NaN there gives 0.  p = 1 drops everything.
+ * out may be x or skip itself with the same strides; the rows of out must not overlap otherwise. */
+#define LSAM_DROPOUT_LAYERS 4096
+#define LSAM_DROPOUT_WORKERS 1048576
+int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, int32_t dtype, int32_t K, int64_t rows, int64_t n, int64_t x_stride_k,
+                 int64_t x_stride_row, int64_t skip_stride_k, int64_t skip_stride_row, int64_t out_stride_k, int64_t out_stride_row, double p,
+                 uint64_t seed, uint64_t tick, int32_t layer, int32_t k_offset, void* cuda_stream, char* h_err, size_t h_err_len);
+
 #ifdef __cplusplus
 }
 #endif

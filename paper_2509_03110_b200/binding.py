@@ -5,6 +5,7 @@ There is no CPU fallback: loading fails loudly when the shared library cannot be
 """
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -27,6 +28,7 @@ EXPORTS = [
     "lsam_profile_enable", "lsam_profile_read", "lsam_launch_count", "lsam_uses_tcgen05", "lsam_last_error",
     "lsam_destroy", "lsam_schedule_hash", "lsam_row_norms_static", "lsam_acc_buffer", "lsam_selftest_bounded_wait",
     "lsam_checkpoint_bytes", "lsam_save_checkpoint", "lsam_load_checkpoint", "lsam_read_anchor_gap",
+    "lsam_logprob", "lsam_logprob_grad", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout",
 ]
 
 
@@ -106,6 +108,13 @@ def lib():
     L.lsam_schedule_hash.restype = C.c_uint64
     L.lsam_schedule_hash.argtypes = [C.c_uint64, C.c_int, C.c_uint64, C.c_uint64, C.c_uint64]
     L.lsam_row_norms_static.argtypes = [vp, C.c_int64, C.c_int64, C.c_int32, vp, vp, C.c_char_p, C.c_size_t]
+    i32, i64, err = C.c_int32, C.c_int64, [vp, C.c_char_p, C.c_size_t]  # err: stream and error buffer
+    L.lsam_logprob.argtypes = [vp, i32, i32] + [i64] * 5 + [vp, i32] + [vp] * 5 + err
+    L.lsam_logprob_grad.argtypes = [vp, i32, i32] + [i64] * 5 + [vp] * 6 + [i64] * 3 + err
+    L.lsam_head_logprob_workspace_bytes.restype = C.c_size_t
+    L.lsam_head_logprob_workspace_bytes.argtypes = [i32, i64, i64]
+    L.lsam_head_logprob.argtypes = [vp, vp, vp, i32, i32] + [i64] * 8 + [vp] * 5 + [C.c_size_t] + err
+    L.lsam_dropout.argtypes = [vp, vp, vp, i32, i32] + [i64] * 8 + [C.c_double, C.c_uint64, C.c_uint64, i32, i32] + err
     _lib = L
     return L
 
@@ -157,6 +166,190 @@ def lsam_row_norms_static(g, n, out, stream=None):
     s = C.c_void_p(stream.cuda_stream) if stream is not None else None
     rc = lib().lsam_row_norms_static(C.c_void_p(g.data_ptr()), ld, int(n), K, C.c_void_p(out.data_ptr()), s, err, 256)
     return int(rc), err.value.decode()
+
+
+# ---- operators around a classifier's head (include/lsam.h, last section)
+FP32, BF16, FP16 = 0, 1, 2
+TOP_MAX, DROPOUT_LAYERS, DROPOUT_WORKERS = 32, 4096, 1 << 20
+
+
+class LogProb(NamedTuple):
+    """Scores of rows of logits: fp32 [..., rows] (top_logp and int32 top_idx: [..., rows, top_k]); None where not asked for."""
+
+    logp: object
+    lse: object
+    entropy: object
+    top_logp: object
+    top_idx: object
+
+
+def _invalid(msg):
+    return LsamError(LSAM_ERR_INVALID, msg)
+
+
+def _stacked(t, what):
+    """(K, rows, columns) and the strides of a [rows, columns] or [K, rows, columns] tensor."""
+    if t.dim() == 2:
+        return (1, *t.shape), (0, *t.stride())
+    if t.dim() == 3:
+        return tuple(t.shape), t.stride()
+    raise _invalid(f"{what} must have 2 or 3 dimensions")
+
+
+def _dtype_code(t, what):
+    name = str(t.dtype)
+    try:
+        return {"torch.float32": FP32, "torch.bfloat16": BF16, "torch.float16": FP16}[name]
+    except KeyError:
+        raise _invalid(f"{what}: {name} is not one of float32, bfloat16, float16") from None
+
+
+def _check_like(t, what, shape, dtype, device):
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or str(t.dtype) != dtype or t.device != device or not t.is_contiguous():
+        raise _invalid(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+class _OnStream:
+    """Allocations inside belong to `stream` (None: the current stream of the device), whose handle is `.handle`."""
+
+    def __init__(self, device, stream):
+        import torch
+
+        if device.type != "cuda":
+            raise _invalid("the operators take CUDA tensors: there is no CPU path")
+        cur = torch.cuda.current_stream(device)
+        self.handle = (stream or cur).cuda_stream
+        self.scope = torch.cuda.stream(stream) if stream is not None and stream != cur else None
+
+    def __enter__(self):
+        if self.scope is not None:
+            self.scope.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+
+
+def _call(fn, *args):
+    err = C.create_string_buffer(256)
+    rc = fn(*args, err, 256)
+    if rc != LSAM_OK:
+        raise LsamError(rc, err.value.decode())
+
+
+def lsam_logprob(logits, labels=None, top_k=0, stream=None):
+    """Log probability of the label, log-sum-exp, entropy and the top_k alternatives of every row of logits.
+
+    logits: [rows, classes] or [K, rows, classes], float32 / bfloat16 / float16, any strides (a context's own logits have the sample
+    index contiguous: a transposed view).  labels: int32 [rows] / [K, rows]; negative = the row is left out (zeros, index -1), None = no
+    logp.  The rules for -inf, NaN and ties stand in include/lsam.h.  Returns LogProb.
+    """
+    import torch
+
+    (K, R, V), (sk, sr, sc) = _stacked(logits, "logits")
+    code = _dtype_code(logits, "logits")
+    lead, dev = logits.shape[:-1], logits.device
+    with _OnStream(dev, stream) as on:
+        pl = _check_like(labels, "labels", lead, "torch.int32", dev)
+        f = torch.empty((3, *lead), dtype=torch.float32, device=dev)
+        tv = ti = None
+        if top_k:
+            if not 0 < top_k <= TOP_MAX:
+                raise _invalid(f"top_k outside 0 .. {TOP_MAX}")
+            tv = torch.empty((*lead, top_k), dtype=torch.float32, device=dev)
+            ti = torch.empty((*lead, top_k), dtype=torch.int32, device=dev)
+        logp, lse, ent = f.unbind(0)
+        _call(lib().lsam_logprob, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, top_k, logp.data_ptr() if pl is not None else None, lse.data_ptr(),
+              ent.data_ptr(), tv.data_ptr() if top_k else None, ti.data_ptr() if top_k else None, on.handle)
+    return LogProb(logp if labels is not None else None, lse, ent, tv, ti)
+
+
+def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, out=None, stream=None):
+    """Gradient with respect to the logits of a loss whose derivatives by logp and entropy are dlogp and dentropy (either may be None).
+
+    lse and entropy: what lsam_logprob returned for these logits.  out: tensor of the logits' shape and type to write (logits itself is
+    allowed), None = a new one.  Returns it.
+    """
+    import torch
+
+    (K, R, V), (sk, sr, sc) = _stacked(logits, "logits")
+    code = _dtype_code(logits, "logits")
+    lead, dev = logits.shape[:-1], logits.device
+    with _OnStream(dev, stream) as on:
+        pl = _check_like(labels, "labels", lead, "torch.int32", dev)
+        rows = [_check_like(t, w, lead, "torch.float32", dev) for t, w in ((lse, "lse"), (entropy, "entropy"), (dlogp, "dlogp"), (dentropy, "dentropy"))]
+        if rows[0] is None:
+            raise _invalid("lse is needed")
+        if out is None:
+            out = torch.empty_like(logits)
+        elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
+            raise _invalid("out must have the shape, type and device of logits")
+        _, (ok, orow, oc) = _stacked(out, "out")
+        _call(lib().lsam_logprob_grad, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, *rows, out.data_ptr(), ok, orow, oc, on.handle)
+    return out
+
+
+def lsam_head_logprob(h, w, labels=None, bias=None, stream=None):
+    """lsam_logprob's first three results for the logits h w^T + bias, without storing them.
+
+    h: [rows, inner] or [K, rows, inner]; w: [classes, inner] (shared by the workers) or [K, classes, inner]; bias: fp32 [classes] /
+    [K, classes]; the inner index contiguous.  Returns LogProb without alternatives.
+    """
+    import torch
+
+    (K, R, D), (hk, hr, hc) = _stacked(h, "h")
+    (KW, V, DW), (wk, wc, wi) = _stacked(w, "w")
+    code = _dtype_code(h, "h")
+    lead, dev = h.shape[:-1], h.device
+    if DW != D or w.dtype != h.dtype or w.device != dev or (w.dim() == 3 and KW != K):
+        raise _invalid("w must be [classes, inner] or [K, classes, inner] of the type and device of h")
+    if (hc != 1 or wi != 1) and D > 1:
+        raise _invalid("the inner index of h and w must be contiguous")
+    with _OnStream(dev, stream) as on:
+        pl = _check_like(labels, "labels", lead, "torch.int32", dev)
+        pb, bk = None, 0
+        if bias is not None:
+            pb = _check_like(bias, "bias", (V,) if bias.dim() == 1 else (K, V), "torch.float32", dev)
+            bk = V if bias.dim() == 2 else 0
+        f = torch.empty((3, *lead), dtype=torch.float32, device=dev)
+        logp, lse, ent = f.unbind(0)
+        nbytes = lib().lsam_head_logprob_workspace_bytes(K, R, V)
+        ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
+        _call(lib().lsam_head_logprob, h.data_ptr(), w.data_ptr(), pb, code, K, R, D, V, hk, hr, wk, wc, bk, pl, logp.data_ptr() if pl is not None else None,
+              lse.data_ptr(), ent.data_ptr(), (ws.data_ptr() + 255) // 256 * 256, nbytes, on.handle)
+    return LogProb(logp if labels is not None else None, lse, ent, None, None)
+
+
+def lsam_dropout(x, p, seed, tick, layer=0, k_offset=0, skip=None, out=None, stream=None):
+    """skip + dropout(x) with a mask that is a function of (seed, tick, layer, worker, row, column) and is never stored.
+
+    x: [rows, n] or [K, rows, n], float32 / bfloat16 / float16, columns contiguous; worker k_offset + k owns x[k].  The backward pass is the
+    same call on the gradient, without skip.  out: tensor to write (x or skip itself is allowed), None = a new one.  Returns it.
+    """
+    import torch
+
+    (K, R, n), (xk, xr, xc) = _stacked(x, "x")
+    code = _dtype_code(x, "x")
+    dev = x.device
+    if not 0 <= int(seed) < 1 << 64 or not 0 <= int(tick) < 1 << 64:
+        raise _invalid("seed and tick are unsigned 64-bit numbers")
+    with _OnStream(dev, stream) as on:
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        for t, what in ((skip, "skip"), (out, "out")):
+            if t is not None and (t.shape != x.shape or t.dtype != x.dtype or t.device != dev):
+                raise _invalid(f"{what} must have the shape, type and device of x")
+        _, (ok, orow, oc) = _stacked(out, "out")
+        (_, (sk, sr, sc)) = _stacked(skip, "skip") if skip is not None else (None, (0, 0, 1))
+        if (xc != 1 or oc != 1 or sc != 1) and n > 1:
+            raise _invalid("the columns of x, skip and out must be contiguous")
+        _call(lib().lsam_dropout, x.data_ptr(), skip.data_ptr() if skip is not None else None, out.data_ptr(), code, K, R, n, xk, xr, sk, sr, ok, orow,
+              p, int(seed), int(tick), int(layer), int(k_offset), on.handle)
+    return out
 
 
 def _np_ptr(a):

@@ -2,12 +2,14 @@
 #pragma once
 
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
 namespace lsam {
 
 typedef __nv_bfloat16 bf16;
+typedef __half fp16;
 
 // Device status word: kernels OR these bits in, the host maps them to error codes.
 enum : int { STATUS_NONFINITE = 1, STATUS_TIMEOUT = 2, STATUS_BAD_INDEX = 4 };
@@ -72,8 +74,10 @@ __device__ inline void langevin_noise4(uint64_t seed, uint64_t t, uint32_t k, ui
 template <typename T> __device__ inline T from_float(float v);
 template <> __device__ inline float from_float<float>(float v) { return v; }
 template <> __device__ inline bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ inline fp16 from_float<fp16>(float v) { return __float2half_rn(v); }
 __device__ inline float to_float(float v) { return v; }
 __device__ inline float to_float(bf16 v) { return __bfloat162float(v); }
+__device__ inline float to_float(fp16 v) { return __half2float(v); }
 
 // ---- fixed-order reductions: xor-shuffle tree inside a warp, then the warp totals are added in warp order
 __device__ inline float warp_sum(float v) {

@@ -1,0 +1,234 @@
+// ops_api.cu -- host side of the operators around a classifier's head (include/lsam.h, last section): argument checks and
+// launches.  Nothing here allocates, synchronises or keeps state between calls.
+#include "lsam.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+
+#include "common.cuh"
+#include "dropout.cuh"
+#include "head_ops.cuh"
+#include "head_score.cuh"
+
+using namespace lsam;
+
+namespace {
+
+struct Err {
+  const char* fn;
+  char* buf;
+  size_t len;
+  Err(const char* f, char* b, size_t n) : fn(f), buf(b), len(n) {
+    if (buf && len > 0) buf[0] = 0;
+  }
+  int fail(int code, const char* msg) const {
+    if (buf && len > 0) std::snprintf(buf, len, "%s: %s", fn, msg);
+    return code;
+  }
+  int launched() const {
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) return LSAM_OK;
+    if (buf && len > 0) std::snprintf(buf, len, "%s: launch failed: %s", fn, cudaGetErrorString(e));
+    return LSAM_ERR_CUDA;
+  }
+};
+
+size_t dtype_size(int32_t d) { return d == LSAM_FP32 ? 4 : 2; }
+bool dtype_ok(int32_t d) { return d == LSAM_FP32 || d == LSAM_BF16 || d == LSAM_FP16; }
+
+// Every pointer a kernel will touch is memory of the current device, aligned to its elements.
+struct PtrCheck {
+  int dev = -1;
+  const char* why = nullptr;
+  PtrCheck() {
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); why = "no current device"; }
+  }
+  void need(const void* p, size_t align) {
+    if (why) return;
+    if (!p) { why = "a required pointer is NULL"; return; }
+    optional(p, align);
+  }
+  void optional(const void* p, size_t align) {
+    if (why || !p) return;
+    if (reinterpret_cast<uintptr_t>(p) % align) { why = "a pointer is not aligned to its element type"; return; }
+    cudaPointerAttributes a;
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) { (void)cudaGetLastError(); why = "a pointer is not device memory"; return; }
+    if (a.type == cudaMemoryTypeManaged) return;
+    if (a.type != cudaMemoryTypeDevice) why = "a pointer is not device memory";
+    else if (a.device != dev) why = "a pointer belongs to another device than the current one";
+  }
+};
+
+constexpr int64_t kMaxIndex = ((int64_t)1 << 31) - 1;
+
+// extents n0 x n1 x n2 with element strides s0, s1, s2: every offset fits a signed 64-bit byte count
+bool strides_ok(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2) {
+  if (s0 < 0 || s1 < 0 || s2 < 0) return false;
+  const __int128 last = (__int128)(n0 - 1) * s0 + (__int128)(n1 - 1) * s1 + (__int128)(n2 - 1) * s2;
+  return last < ((__int128)1 << 60);
+}
+
+template <class F>
+void by_dtype(int32_t d, F&& f) {
+  if (d == LSAM_FP32) f(float());
+  else if (d == LSAM_BF16) f(bf16());
+  else f(fp16());
+}
+
+}  // namespace
+
+extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                            int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
+                            float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len) {
+  const Err err("lsam_logprob", h_err, h_err_len);
+  if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
+  if (K < 0 || rows < 0 || classes < 1 || classes > kMaxIndex) return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= classes < 2^31");
+  if (top_k < 0 || top_k > LSAM_TOP_MAX) return err.fail(LSAM_ERR_INVALID, "top_k outside 0 .. LSAM_TOP_MAX");
+  if (d_logp && !d_labels) return err.fail(LSAM_ERR_INVALID, "d_logp without d_labels");
+  if (K == 0 || rows == 0) return LSAM_OK;
+  if (rows > kMaxIndex / K) return err.fail(LSAM_ERR_INVALID, "K * rows must be below 2^31");
+  if (!strides_ok(K, stride_k, rows, stride_row, classes, stride_class)) return err.fail(LSAM_ERR_INVALID, "a stride is negative or the tensor is too large");
+  PtrCheck pc;
+  pc.need(d_logits, dtype_size(dtype));
+  pc.optional(d_labels, 4); pc.optional(d_logp, 4); pc.optional(d_lse, 4); pc.optional(d_entropy, 4);
+  if (top_k > 0) { pc.need(d_top_logp, 4); pc.need(d_top_idx, 4); }
+  if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
+  const ScoreOut out{d_logp, d_lse, d_entropy, d_top_logp, d_top_idx, top_k};
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const int64_t total = (int64_t)K * rows;
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes};
+    logprob_kernel<T><<<(unsigned)total, 256, 0, stream>>>(v, d_labels, out);
+  });
+  return err.launched();
+}
+
+extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                                 int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
+                                 const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
+                                 void* cuda_stream, char* h_err, size_t h_err_len) {
+  const Err err("lsam_logprob_grad", h_err, h_err_len);
+  if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
+  if (K < 0 || rows < 0 || classes < 1 || classes > kMaxIndex) return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= classes < 2^31");
+  if (!d_dlogp && !d_dentropy) return err.fail(LSAM_ERR_INVALID, "neither d_dlogp nor d_dentropy is given");
+  if (d_dlogp && !d_labels) return err.fail(LSAM_ERR_INVALID, "d_dlogp without d_labels");
+  if (d_dentropy && !d_entropy) return err.fail(LSAM_ERR_INVALID, "d_dentropy without d_entropy");
+  if (K == 0 || rows == 0) return LSAM_OK;
+  if (rows > kMaxIndex / K) return err.fail(LSAM_ERR_INVALID, "K * rows must be below 2^31");
+  if (!strides_ok(K, stride_k, rows, stride_row, classes, stride_class) || !strides_ok(K, out_stride_k, rows, out_stride_row, classes, out_stride_class))
+    return err.fail(LSAM_ERR_INVALID, "a stride is negative or the tensor is too large");
+  if ((K > 1 && out_stride_k == 0) || (rows > 1 && out_stride_row == 0) || (classes > 1 && out_stride_class == 0))
+    return err.fail(LSAM_ERR_INVALID, "elements of the gradient share an address");
+  PtrCheck pc;
+  pc.need(d_logits, dtype_size(dtype)); pc.need(d_dlogits, dtype_size(dtype)); pc.need(d_lse, 4);
+  pc.optional(d_labels, 4); pc.optional(d_entropy, 4); pc.optional(d_dlogp, 4); pc.optional(d_dentropy, 4);
+  if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
+  const GradIn in{d_labels, d_lse, d_entropy, d_dlogp, d_dentropy};
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const int64_t total = (int64_t)K * rows;
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes};
+    const GradOut<T> o{static_cast<T*>(d_dlogits), out_stride_k, out_stride_row, out_stride_class};
+    logprob_grad_kernel<T><<<(unsigned)total, 256, 0, stream>>>(v, in, o);
+  });
+  return err.launched();
+}
+
+namespace {
+
+// How a head call is cut: enough shares of the classes to occupy the machine, none shorter than a few tiles.
+struct HeadPlan {
+  int splits = 1;
+  int64_t per_split = 0;
+};
+HeadPlan head_plan(int32_t K, int64_t rows, int64_t classes) {
+  HeadPlan p;
+  const int64_t blocks = (int64_t)K * ceil_div(rows, kHsM);
+  int64_t splits = std::min<int64_t>(ceil_div(2 * 148, blocks), ceil_div(classes, kHsN));
+  p.per_split = round_up(ceil_div(classes, std::max<int64_t>(splits, 1)), kHsN);
+  p.splits = (int)ceil_div(classes, p.per_split);
+  return p;
+}
+size_t head_bytes(const HeadPlan& p, int64_t total) { return (size_t)round_up((int64_t)sizeof(RowStat) * p.splits * total, 256) + 4 * (size_t)total; }
+
+}  // namespace
+
+extern "C" size_t lsam_head_logprob_workspace_bytes(int32_t K, int64_t rows, int64_t classes) {
+  if (K < 1 || rows < 1 || classes < 1 || rows > kMaxIndex / K || classes > kMaxIndex) return 0;
+  return head_bytes(head_plan(K, rows, classes), (int64_t)K * rows);
+}
+
+extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
+                                 int64_t h_stride_k, int64_t h_stride_row, int64_t w_stride_k, int64_t w_stride_class, int64_t bias_stride_k,
+                                 const int32_t* d_labels, float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes,
+                                 void* cuda_stream, char* h_err, size_t h_err_len) {
+  const Err err("lsam_head_logprob", h_err, h_err_len);
+  if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
+  if (K < 0 || rows < 0 || inner < 1 || classes < 1 || classes > kMaxIndex || inner > kMaxIndex)
+    return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= inner, classes < 2^31");
+  if (d_logp && !d_labels) return err.fail(LSAM_ERR_INVALID, "d_logp without d_labels");
+  if (K == 0 || rows == 0) return LSAM_OK;
+  if (K > 65535 || rows > kMaxIndex / K || rows > (int64_t)kHsM * 65535) return err.fail(LSAM_ERR_INVALID, "need K <= 65535, rows <= 4194240, K * rows < 2^31");
+  if (!strides_ok(K, h_stride_k, rows, h_stride_row, inner, 1) || !strides_ok(K, w_stride_k, classes, w_stride_class, inner, 1) || bias_stride_k < 0)
+    return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
+  const HeadPlan plan = head_plan(K, rows, classes);
+  const int64_t total = (int64_t)K * rows;
+  if (workspace_bytes < head_bytes(plan, total)) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_head_logprob_workspace_bytes()");
+  if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return err.fail(LSAM_ERR_WORKSPACE, "workspace not 256-byte aligned");
+  PtrCheck pc;
+  pc.need(d_h, dtype_size(dtype)); pc.need(d_w, dtype_size(dtype)); pc.need(d_workspace, 256);
+  pc.optional(d_bias, 4); pc.optional(d_labels, 4); pc.optional(d_logp, 4); pc.optional(d_lse, 4); pc.optional(d_entropy, 4);
+  if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
+  HeadArgs a{rows, inner, classes, h_stride_k, h_stride_row, w_stride_k, w_stride_class, bias_stride_k, d_bias, d_labels, plan.splits, plan.per_split,
+             static_cast<RowStat*>(d_workspace),
+             reinterpret_cast<float*>(static_cast<char*>(d_workspace) + round_up((int64_t)sizeof(RowStat) * plan.splits * total, 256))};
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    head_score_simt_kernel<T><<<dim3((unsigned)plan.splits, (unsigned)ceil_div(rows, kHsM), (unsigned)K), 256, 0, stream>>>(static_cast<const T*>(d_h), static_cast<const T*>(d_w), a);
+  });
+  const ScoreOut out{d_logp, d_lse, d_entropy, nullptr, nullptr, 0};
+  head_join_kernel<<<(unsigned)ceil_div(total, 128), 128, 0, stream>>>(a, total, out);
+  return err.launched();
+}
+
+extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, int32_t dtype, int32_t K, int64_t rows, int64_t n, int64_t x_stride_k,
+                            int64_t x_stride_row, int64_t skip_stride_k, int64_t skip_stride_row, int64_t out_stride_k, int64_t out_stride_row, double p,
+                            uint64_t seed, uint64_t tick, int32_t layer, int32_t k_offset, void* cuda_stream, char* h_err, size_t h_err_len) {
+  const Err err("lsam_dropout", h_err, h_err_len);
+  if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
+  if (!(p >= 0.0 && p <= 1.0)) return err.fail(LSAM_ERR_INVALID, "p outside [0, 1]");
+  if (K < 0 || rows < 0 || n < 0) return err.fail(LSAM_ERR_INVALID, "a negative size");
+  if (layer < 0 || layer >= LSAM_DROPOUT_LAYERS) return err.fail(LSAM_ERR_INVALID, "layer outside 0 .. LSAM_DROPOUT_LAYERS - 1");
+  if (k_offset < 0 || (int64_t)k_offset + K > LSAM_DROPOUT_WORKERS) return err.fail(LSAM_ERR_INVALID, "workers outside 0 .. LSAM_DROPOUT_WORKERS - 1");
+  if (K == 0 || rows == 0 || n == 0) return LSAM_OK;
+  if (rows > kMaxIndex || n > kMaxIndex) return err.fail(LSAM_ERR_INVALID, "rows and n must be below 2^31");
+  if (!strides_ok(K, x_stride_k, rows, x_stride_row, n, 1) || !strides_ok(K, out_stride_k, rows, out_stride_row, n, 1) ||
+      (d_skip && !strides_ok(K, skip_stride_k, rows, skip_stride_row, n, 1)))
+    return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
+  if ((K > 1 && out_stride_k == 0) || (rows > 1 && out_stride_row < n)) return err.fail(LSAM_ERR_INVALID, "elements of the output share an address");
+  const int64_t groups = ceil_div(n, 8);
+  if ((__int128)groups * rows * K >= ((__int128)1 << 38)) return err.fail(LSAM_ERR_INVALID, "K * rows * ceil(n / 8) must be below 2^38");
+  PtrCheck pc;
+  pc.need(d_x, dtype_size(dtype)); pc.need(d_out, dtype_size(dtype)); pc.optional(d_skip, dtype_size(dtype));
+  if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
+  DropArgs a;
+  a.rows = rows; a.n = n;
+  a.xk = x_stride_k; a.xr = x_stride_row; a.sk = skip_stride_k; a.sr = skip_stride_row; a.ok = out_stride_k; a.orr = out_stride_row;
+  a.key0 = (uint32_t)seed ^ 0x64726f70u;  // "drop"
+  a.key1 = (uint32_t)(seed >> 32) ^ (uint32_t)(tick >> 32);
+  a.tick = (uint32_t)tick;
+  a.word2 = ((uint32_t)layer << 20) + (uint32_t)k_offset;
+  a.cut = (uint32_t)std::floor(p * 65536.0 + 0.5);
+  a.scale = a.cut < 65536u ? 65536.f / (float)(65536u - a.cut) : 0.f;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const int64_t total = groups * rows * K;
+  by_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    dropout_kernel<T><<<(unsigned)ceil_div(total, 256), 256, 0, stream>>>(static_cast<const T*>(d_x), static_cast<const T*>(d_skip), static_cast<T*>(d_out), a, groups, total);
+  });
+  return err.launched();
+}

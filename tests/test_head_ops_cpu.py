@@ -1,0 +1,102 @@
+"""Refusals of the operators around a classifier's head that need no GPU: every bad argument is turned into an error code on the host."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2509_03110_b200 import binding as G
+
+P = C.c_void_p(1 << 20)  # never dereferenced: each call below is refused before any pointer is used
+
+
+def _call(fn, *args):
+    err = C.create_string_buffer(256)
+    rc = fn(*args, None, err, 256)
+    return rc, err.value.decode()
+
+
+def _logprob(dtype=0, K=1, rows=2, classes=5, sk=10, sr=5, sc=1, labels=P, top_k=0, logp=P):
+    return _call(G.lib().lsam_logprob, P, dtype, K, rows, classes, sk, sr, sc, labels, top_k, logp, P, P, P, P)
+
+
+def _grad(dtype=0, K=1, rows=2, classes=5, sk=10, sr=5, sc=1, labels=P, entropy=P, dlogp=P, dentropy=P, ok=10, orow=5, oc=1):
+    return _call(G.lib().lsam_logprob_grad, P, dtype, K, rows, classes, sk, sr, sc, labels, P, entropy, dlogp, dentropy, P, ok, orow, oc)
+
+
+def _head(dtype=1, K=1, rows=2, inner=8, classes=5, hr=8, wc=8, bk=0, labels=P, ws=P, nbytes=1 << 20):
+    return _call(G.lib().lsam_head_logprob, P, P, None, dtype, K, rows, inner, classes, 16, hr, 40, wc, bk, labels, P, P, P, ws, nbytes)
+
+
+def _dropout(dtype=0, K=1, rows=2, n=5, xr=5, orow=5, ok=10, p=0.5, layer=0, k_offset=0):
+    return _call(G.lib().lsam_dropout, P, None, P, dtype, K, rows, n, 10, xr, 0, 0, ok, orow, p, 1, 2, layer, k_offset)
+
+
+@pytest.mark.parametrize("kw, word", [
+    (dict(dtype=3), "dtype"), (dict(dtype=-1), "dtype"), (dict(K=-1), "K >= 0"), (dict(rows=-1), "rows >= 0"), (dict(classes=0), "classes"),
+    (dict(classes=1 << 31), "classes"), (dict(top_k=-1), "top_k"), (dict(top_k=33), "top_k"), (dict(labels=None), "d_labels"),
+    (dict(K=1 << 16, rows=1 << 16), "2^31"), (dict(sr=-5), "stride"), (dict(sk=1 << 62, K=3), "stride"), (dict(sr=1 << 61, rows=2), "stride")])
+def test_logprob_refuses(kw, word):
+    rc, msg = _logprob(**kw)
+    assert rc == G.LSAM_ERR_INVALID and word in msg and msg.startswith("lsam_logprob: "), (rc, msg)
+
+
+@pytest.mark.parametrize("kw, word", [
+    (dict(dtype=7), "dtype"), (dict(classes=0), "classes"), (dict(dlogp=None, dentropy=None), "neither"), (dict(labels=None), "d_labels"), (dict(entropy=None), "d_entropy"),
+    (dict(sc=-1), "stride"), (dict(orow=-1), "stride"), (dict(orow=0), "address"), (dict(oc=0), "address"), (dict(K=2, ok=0), "address"), (dict(K=1 << 16, rows=1 << 16), "2^31")])
+def test_grad_refuses(kw, word):
+    rc, msg = _grad(**kw)
+    assert rc == G.LSAM_ERR_INVALID and word in msg, (rc, msg)
+
+
+@pytest.mark.parametrize("kw, code, word", [
+    (dict(dtype=5), G.LSAM_ERR_INVALID, "dtype"), (dict(inner=0), G.LSAM_ERR_INVALID, "inner"), (dict(classes=0), G.LSAM_ERR_INVALID, "classes"), (dict(labels=None), G.LSAM_ERR_INVALID, "d_labels"),
+    (dict(K=65536), G.LSAM_ERR_INVALID, "65535"), (dict(rows=4194241), G.LSAM_ERR_INVALID, "4194240"), (dict(hr=-8), G.LSAM_ERR_INVALID, "stride"), (dict(bk=-1), G.LSAM_ERR_INVALID, "stride"),
+    (dict(nbytes=4), G.LSAM_ERR_WORKSPACE, "workspace"), (dict(ws=C.c_void_p((1 << 20) + 16)), G.LSAM_ERR_WORKSPACE, "aligned")])
+def test_head_refuses(kw, code, word):
+    rc, msg = _head(**kw)
+    assert rc == code and word in msg, (rc, msg)
+
+
+@pytest.mark.parametrize("kw, word", [
+    (dict(dtype=3), "dtype"), (dict(p=-0.1), "p outside"), (dict(p=1.01), "p outside"), (dict(p=float("nan")), "p outside"), (dict(n=-1), "negative"), (dict(layer=-1), "layer"), (dict(layer=4096), "layer"),
+    (dict(k_offset=-1), "workers"), (dict(k_offset=(1 << 20) - 1, K=2), "workers"), (dict(n=1 << 31), "2^31"), (dict(xr=-1), "stride"), (dict(orow=4), "address"), (dict(K=2, ok=0), "address"),
+    (dict(rows=(1 << 31) - 1, n=(1 << 31) - 1, orow=(1 << 31) - 1, xr=0), "stride|2^38")])
+def test_dropout_refuses(kw, word):
+    rc, msg = _dropout(**kw)
+    assert rc == G.LSAM_ERR_INVALID and any(w in msg for w in word.split("|")), (rc, msg)
+
+
+def test_empty_calls_do_nothing():
+    for kw in (dict(K=0), dict(rows=0)):
+        assert _logprob(**kw)[0] == G.LSAM_OK and _grad(**kw)[0] == G.LSAM_OK and _head(**kw)[0] == G.LSAM_OK and _dropout(**kw)[0] == G.LSAM_OK
+    assert _dropout(n=0)[0] == G.LSAM_OK
+
+
+def test_host_pointers_are_refused():
+    # without a GPU there is no current device; with one, these addresses are not device memory
+    for call in (_logprob, _grad, _head, _dropout):
+        rc, msg = call()
+        assert rc == G.LSAM_ERR_INVALID and ("device" in msg or "pointer" in msg), msg
+
+
+def test_error_buffer_is_optional():
+    assert G.lib().lsam_dropout(P, None, P, 9, 1, 1, 1, 1, 1, 0, 0, 1, 1, 0.5, 1, 1, 0, 0, None, None, 0) == G.LSAM_ERR_INVALID
+
+
+def test_workspace_bytes_grow_with_the_rows():
+    f = G.lib().lsam_head_logprob_workspace_bytes
+    assert f(0, 1, 1) == 0 and f(1, 0, 1) == 0 and f(1, 1, 0) == 0
+    assert 0 < f(1, 1, 1) <= f(1, 4096, 32768) and f(32, 256, 1000) >= 32 * 256 * 16
+
+
+def test_binding_refuses_what_is_not_a_cuda_tensor_of_the_right_form():
+    x = torch.zeros(2, 8)
+    for call in (lambda: G.lsam_logprob(x), lambda: G.lsam_dropout(x, 0.5, 1, 1), lambda: G.lsam_head_logprob(x, x), lambda: G.lsam_logprob_grad(x, None, None, None)):
+        with pytest.raises(G.LsamError) as e:
+            call()
+        assert e.value.code == G.LSAM_ERR_INVALID
+    for bad in (torch.zeros(8), torch.zeros(1, 2, 3, 4), torch.zeros(2, 8, dtype=torch.float64)):
+        with pytest.raises(G.LsamError):
+            G.lsam_logprob(bad)
+    with pytest.raises(G.LsamError):
+        G.lsam_dropout(x, 0.5, -1, 1)
