@@ -329,9 +329,9 @@ enum { LSAM_FP32 = 0, LSAM_BF16 = 1, LSAM_FP16 = 2 };
  *  d_labels   nullable int32: a negative label leaves the row out (it is not read; logp = lse = entropy = 0, no alternatives); a
  *             label >= classes makes logp NaN.
  *  d_logp (needs d_labels), d_lse, d_entropy: nullable.  top_k = 0 .. LSAM_TOP_MAX; with 0 the two top arrays are not touched.
- * Logits of -inf have probability 0 and are never alternatives: missing alternatives have index -1 and log probability -inf, a row with
- * nothing but -inf has lse = -inf, logp = -inf, entropy 0.  A NaN or a +inf logit makes lse, entropy and every log probability of its row
- * NaN (a label of logit -inf keeps -inf); NaN is never an alternative. */
+ * Logits below -1e30 are masks (-inf, or the lowest value of bf16 and fp32): probability 0, log probability -inf, never alternatives.
+ * Missing alternatives have index -1 and log probability -inf; a row of nothing but masks has lse = -inf, logp = -inf, entropy 0.  A NaN or a
+ * +inf logit (from 2e38 on) makes lse, entropy and every log probability of its row NaN (a masked label keeps -inf); NaN is never an alternative. */
 #define LSAM_TOP_MAX 32
 int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                  int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
@@ -342,7 +342,7 @@ int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, i
  * with lse and entropy [K, rows] as lsam_logprob returned them for the same logits, dlogp and dentropy [K, rows] the loss's derivatives
  * (nullable: 0; not both NULL; dlogp needs d_labels, dentropy needs d_entropy).  The minibatch cross-entropy of a context is
  * dlogp = -1 / batch.  Rows that are left out (negative label) and rows of nothing but
- * masks (lse below -1e30: every logit -inf, or the lowest value of a type) get zeros; a label >= classes makes its row NaN.
+ * masks (lse = -inf) get zeros; a label >= classes makes its row NaN.
  * d_dlogits: type of the logits, strides of its own (no two elements at one address); may be d_logits itself with the same strides. */
 int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                       int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,

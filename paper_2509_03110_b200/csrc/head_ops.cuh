@@ -6,7 +6,7 @@
 
 namespace lsam {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f;  // log2 e, rounded
 constexpr int kTopMax = 32;  // most alternatives a call returns (LSAM_TOP_MAX)
 
 // 2^x, one instruction on the special-function unit (relative error below 2^-22; results below 2^-126 are flushed to 0)
@@ -16,21 +16,34 @@ __device__ inline float ex2(float x) {
   return y;
 }
 
-// Running statistics of a set of logits: m = maximum (NaN ignored), s = sum e^(l - m), t = sum e^(l - m) (l - m), so that
-//   logsumexp = m + log s,   entropy = -sum p log p = log s - t / s.
-// A set with nothing but -inf has m = -inf, s = t = 0; a NaN or a +inf makes s NaN.  Differences below kFloor are cut there:
-// e^kFloor is 0 in 32 bits, and (-inf) * 0 never arises.
-constexpr float kFloor = -200.f;
+// Running statistics of a set of logits, held relative to its maximum m (NaN ignored) in units of log 2.  With k = kLog2e, B = fl(m k)
+// and w = l k - B (one fused multiply-add):  s = sum 2^w,  t = sum 2^w w,  so that
+//   logsumexp = m + (log2 s - (m k - B)) / k,   entropy = -sum p log p = (log2 s - t / s) / k.
+// B is the reference itself, not an approximation of m k, and k's own rounding only scales the logits by 1 + 1e-8: an offset common to all
+// logits costs no digits of the entropy or of a log probability.  Logits below kMasked are masks: they enter as kMasked, whose 2^w is 0
+// beside any other (and (-inf) * 0 never arises); a set of nothing but masks has m = kMasked.  A NaN or +inf logit makes s NaN.
+constexpr float kMasked = -1e30f;
 struct RowStat { float m, s, t; };
-__device__ inline float stat_base(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ inline RowStat stat_empty() { return {-INFINITY, 0.f, 0.f}; }
-__device__ inline void stat_rebase(RowStat& a, float m) {  // m >= a.m: express a's sums relative to m
-  if (a.m == -INFINITY) { a.m = m; return; }               // s is 0, or NaN from a NaN logit
-  const float d = fmaxf(a.m - m, kFloor);
-  const float f = ex2(d * kLog2e);
+__device__ inline float max_nan(float a, float b) {  // NaN if either is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ inline RowStat stat_empty() { return {kMasked, 0.f, 0.f}; }
+__device__ inline void stat_rebase(RowStat& a, float m) {  // express a's sums relative to m >= a.m
+  const float d = __fmul_rn(a.m, kLog2e) - __fmul_rn(m, kLog2e);  // the difference of the two references: never contracted
+  const float f = ex2(d);
   a.t = f * fmaf(d, a.s, a.t);
   a.s *= f;
   a.m = m;
+}
+__device__ inline void stat_add(RowStat& a, float l) {  // one logit, masks and NaN included
+  l = max_nan(l, kMasked);
+  if (l > a.m) stat_rebase(a, l);
+  const float w = fmaf(l, kLog2e, -(a.m * kLog2e));
+  const float e = ex2(w);
+  a.s += e;
+  a.t = fmaf(e, w, a.t);
 }
 __device__ inline RowStat stat_merge(RowStat a, RowStat b) {
   const float m = fmaxf(a.m, b.m);
@@ -38,24 +51,26 @@ __device__ inline RowStat stat_merge(RowStat a, RowStat b) {
   stat_rebase(b, m);
   return {m, a.s + b.s, a.t + b.t};
 }
-struct RowScore { float base, ls, lse, ent; };  // lse = base + ls
-__device__ inline RowScore stat_finish(const RowStat& a) {
-  if (a.m == -INFINITY && a.s == 0.f) return {0.f, -INFINITY, -INFINITY, 0.f};
-  const float base = stat_base(a.m), ls = logf(a.s);
-  return {base, ls, base + ls, ls - a.t / a.s};
+__device__ inline RowStat stat_shfl_xor(const RowStat& a, int d) {
+  return {__shfl_xor_sync(~0u, a.m, d), __shfl_xor_sync(~0u, a.s, d), __shfl_xor_sync(~0u, a.t, d)};
 }
-// log probability of a class, relative to the maximum: a large common offset of the logits costs no digits
-__device__ inline float score_logp(float l, const RowScore& r) { return l == -INFINITY ? l : (l - r.base) - r.ls; }
+struct RowScore { float B, ls, lse, ent; };
+__device__ inline RowScore stat_finish(const RowStat& a) {
+  if (a.m <= kMasked && a.s == a.s) return {0.f, 0.f, -INFINITY, 0.f};
+  const float B = a.m * kLog2e, ls = log2f(a.s);
+  return {B, ls, a.m + (ls - fmaf(a.m, kLog2e, -B)) / kLog2e, (ls - a.t / a.s) / kLog2e};
+}
+__device__ inline float score_logp(float l, const RowScore& r) { return l < kMasked ? -INFINITY : (fmaf(l, kLog2e, -r.B) - r.ls) / kLog2e; }
 
 // Order of the alternatives: larger logit first, then the lower class.  One 64-bit key per element (0: not an alternative,
-// i.e. -inf or NaN); -0 and +0 are one value.
+// i.e. a mask or NaN); -0 and +0 are one value.
 __device__ inline uint32_t order_bits(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 __device__ inline float order_value(uint32_t o) { return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
 __device__ inline uint64_t order_key(float v, int32_t c) {
-  return v > -INFINITY ? ((uint64_t)order_bits(v) << 32) | (uint32_t)~c : 0ull;
+  return v >= kMasked ? ((uint64_t)order_bits(v) << 32) | (uint32_t)~c : 0ull;
 }
 
 // Logits of one call: element (k, r, c) at p[k * sk + r * sr + c * sc]; row index = k * rows + r.
@@ -100,19 +115,8 @@ logprob_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o) {
   }
   const T* row = v.row(i);
   RowStat a = stat_empty();
-  for (int c = tid; c < v.classes; c += 256) {
-    const float l = to_float(row[c * v.sc]);
-    if (l > a.m) stat_rebase(a, l);
-    float u = l - stat_base(a.m);
-    u = u < kFloor ? kFloor : u;
-    const float e = ex2(u * kLog2e);
-    a.s += e;
-    a.t = fmaf(e, u, a.t);
-  }
-  for (int d = 16; d > 0; d >>= 1) {
-    RowStat b = {__shfl_xor_sync(~0u, a.m, d), __shfl_xor_sync(~0u, a.s, d), __shfl_xor_sync(~0u, a.t, d)};
-    a = stat_merge(a, b);
-  }
+  for (int c = tid; c < v.classes; c += 256) stat_add(a, to_float(row[c * v.sc]));
+  for (int d = 16; d > 0; d >>= 1) a = stat_merge(a, stat_shfl_xor(a, d));
   if (lane == 0) ws[w] = a;
   __syncthreads();
   a = ws[0];
@@ -148,9 +152,7 @@ logprob_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o) {
 }
 
 // Gradient of L(logp, entropy) of every row:  dl_c = a (1[c = y] - p_c) - b p_c (log p_c + H),  p_c = e^(l_c - lse),
-// a = dL/dlogp, b = dL/dH (each nullable = 0).  Rows that are left out (y < 0) or hold nothing but masks (lse below kMaskedLse: -inf, or the
-// lowest value of a type, beside which log classes is lost) get 0.
-constexpr float kMaskedLse = -1e30f;
+// a = dL/dlogp, b = dL/dH (each nullable = 0).  Rows that are left out (y < 0) or hold nothing but masks (lse = -inf) get 0.
 struct GradIn {
   const int32_t* labels;
   const float *lse, *entropy, *dlogp, *dentropy;
@@ -165,15 +167,14 @@ logprob_grad_kernel(LogitView<T> v, GradIn g, GradOut<T> out) {
   const int32_t y = g.labels ? g.labels[i] : v.classes - 1;
   const float lse = g.lse[i];
   T* dst = out.p + (i / v.rows) * out.sk + (i % v.rows) * out.sr;
-  const bool none = y < 0 || lse < kMaskedLse;
+  const bool none = y < 0 || lse < kMasked;
   const T* row = v.row(i);
   const float a = g.dlogp ? g.dlogp[i] : 0.f, b = g.dentropy ? g.dentropy[i] : 0.f, H = g.dentropy ? g.entropy[i] : 0.f;
   const float bad = y >= v.classes ? NAN : 0.f;
   for (int c = threadIdx.x; c < v.classes; c += 256) {
     float d = 0.f;
     if (!none) {
-      float u = to_float(row[c * v.sc]) - lse;
-      u = u < kFloor ? kFloor : u;
+      const float u = max_nan(to_float(row[c * v.sc]), kMasked) - lse;
       const float p = ex2(u * kLog2e);
       d = a * ((c == y ? 1.f : 0.f) - p) - b * (p * (u + H)) + bad;
     }

@@ -8,13 +8,13 @@
 namespace lsam {
 
 struct HeadArgs {
-  int64_t rows, inner, classes;
+  int64_t rows, inner, classes, total;  // total = K * rows
   int64_t hk, hr, wk, wr, bk;  // strides: h worker / row, w worker / class, bias worker (the contraction index is contiguous)
   const float* bias;           // nullable
   const int32_t* labels;       // nullable
-  int splits;                  // shares of the classes, each left to one block
-  int64_t per_split;           // classes of a share
-  RowStat* part;               // [splits][K * rows]
+  int parts;                   // partial statistics per row
+  int64_t per_split;           // SIMT form: classes of a block's share
+  RowStat* part;               // [parts][K * rows]
   float* at_label;             // [K * rows] logit of the label
 };
 
@@ -27,6 +27,7 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 head_score_simt_kernel(const T* __restrict__ h, const T* __restrict__ w, HeadArgs a) {
   __shared__ float hs[kHsK][kHsM + 4], wsm[kHsK][kHsN + 4];
+  grid_dep_launch();  // the join may become resident; it waits for this grid
   const int64_t k = blockIdx.z, r0 = (int64_t)blockIdx.y * kHsM;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const int64_t c_begin = (int64_t)blockIdx.x * a.per_split, c_end = min(a.classes, c_begin + a.per_split);
@@ -70,45 +71,49 @@ head_score_simt_kernel(const T* __restrict__ h, const T* __restrict__ w, HeadArg
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float l = acc[i][j] + b;
-        if (l > st[i].m) stat_rebase(st[i], l);
-        float u = l - stat_base(st[i].m);
-        u = u < kFloor ? kFloor : u;
-        const float e = ex2(u * kLog2e);
-        st[i].s += e;
-        st[i].t = fmaf(e, u, st[i].t);
+        stat_add(st[i], l);
         if (c == y[i]) a.at_label[k * a.rows + r0 + ty * 4 + i] = l;  // y is -1 in rows beyond the last
       }
     }
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    for (int d = 8; d > 0; d >>= 1) {
-      RowStat b = {__shfl_xor_sync(~0u, st[i].m, d), __shfl_xor_sync(~0u, st[i].s, d), __shfl_xor_sync(~0u, st[i].t, d)};
-      st[i] = stat_merge(st[i], b);
-    }
+    for (int d = 8; d > 0; d >>= 1) st[i] = stat_merge(st[i], stat_shfl_xor(st[i], d));
     const int64_t r = r0 + ty * 4 + i;
     if (tx == 0 && r < a.rows) a.part[((int64_t)blockIdx.x * gridDim.z + k) * a.rows + r] = st[i];
   }
 }
 
-// Joins the shares of a row in ascending order.  One thread per row.
-__global__ void __launch_bounds__(128)
+// Joins the partial statistics of a row in a fixed order: 32 rows per block (threadIdx.x), partials y, y + 32, ... per thread, then the 32
+// sums in ascending order of a tree.  grid ceil(total / 32), block (32, 32)
+__global__ void __launch_bounds__(1024)
 head_join_kernel(HeadArgs a, int64_t total, ScoreOut o) {
-  const int64_t i = (int64_t)blockIdx.x * 128 + threadIdx.x;
-  if (i >= total) return;
-  const int32_t y = a.labels ? a.labels[i] : 0;
+  grid_dep_wait();
+  __shared__ float red[3][32][33];
+  const int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  RowStat st = stat_empty();
+  if (i < total)
+    for (int p = threadIdx.y; p < a.parts; p += 32) st = stat_merge(st, a.part[(int64_t)p * total + i]);
+  red[0][threadIdx.y][threadIdx.x] = st.m;
+  red[1][threadIdx.y][threadIdx.x] = st.s;
+  red[2][threadIdx.y][threadIdx.x] = st.t;
+  __syncthreads();
+  // turned: warp y joins row y of the block over its 32 lanes
+  st = {red[0][threadIdx.x][threadIdx.y], red[1][threadIdx.x][threadIdx.y], red[2][threadIdx.x][threadIdx.y]};
+  for (int d = 16; d > 0; d >>= 1) st = stat_merge(st, stat_shfl_xor(st, d));
+  const int64_t r = (int64_t)blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x != 0 || r >= total) return;
+  const int32_t y = a.labels ? a.labels[r] : 0;
   float lse = 0.f, ent = 0.f, lp = 0.f;
   if (y >= 0) {
-    RowStat st = a.part[i];
-    for (int s = 1; s < a.splits; ++s) st = stat_merge(st, a.part[(int64_t)s * total + i]);
     const RowScore sc = stat_finish(st);
     lse = sc.lse;
     ent = sc.ent;
-    if (o.logp) lp = y < a.classes ? score_logp(a.at_label[i], sc) : NAN;
+    if (o.logp) lp = y < a.classes ? score_logp(a.at_label[r], sc) : NAN;
   }
-  if (o.logp) o.logp[i] = lp;
-  if (o.lse) o.lse[i] = lse;
-  if (o.entropy) o.entropy[i] = ent;
+  if (o.logp) o.logp[r] = lp;
+  if (o.lse) o.lse[r] = lse;
+  if (o.entropy) o.entropy[r] = ent;
 }
 
 }  // namespace lsam

@@ -1,0 +1,336 @@
+// head_tcgen05.cuh -- scores of activations against a head on the 5th-generation tensor cores: the logits of a tile live in tensor
+// memory only, and the warps that drain them keep the row statistics of head_ops.cuh instead of storing them.
+//
+// D(row, class) = sum_i h(row, i) w(class, i): rows on the M side, so a thread that drains tensor memory owns ONE row (its lane) and walks
+// the classes of the tile in registers: no exchange between threads, the maximum, sum and entropy sum of a row stay in three registers over
+// a run of tiles.  TMA stages 128B-swizzled tiles of 64 inner indices, one thread issues tcgen05.mma, eight warps drain (two per lane
+// quadrant, alternate pairs of 32 columns); the accumulator is double-buffered so that a tile's statistics hide behind the next tile's products.
+//   PAIR (more than 128 rows): two CTAs share 256 rows x tile_n classes (cta_group::2), each staging its own 128 rows of h and half the
+//     classes; what bounds a CTA is the rate at which it takes in operands, 32 KB per 256 x 256 x 64 block instead of 48.
+//   single CTA (up to 128 rows): the bytes of w bound it; only the rows that exist are loaded (the others' accumulator rows are never read).
+// tile_n, a multiple of 32 up to 256, is the width that loads all SMs evenly.  The work list has the row tile fastest: the CTAs that run together
+// read the same few tiles of w, so w crosses HBM once, whatever the number of row tiles.
+// All waits are bounded as in gemm_tcgen05.cuh; a CTA that gives up leaves NaN statistics for its rows.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.cuh"
+#include "head_score.cuh"
+#include "tc_ptx.cuh"
+
+namespace lsam {
+
+// warp 0: TMA producer, warp 1: MMA issuer and tensor-memory owner, warps 2, 3: none; warps 4-11: draining.  A draining thread holds the 128
+// logits of its row's half tile, so the registers go to those two warpgroups: 56 + 2 x 216 a thread out of the 3 x 168 of the launch.
+constexpr int kHtThreads = 384;
+constexpr int kHtRegsIssue = 56, kHtRegsDrain = 216;
+static_assert((kHtRegsIssue + 2 * kHtRegsDrain) * 128 <= 168 * kHtThreads, "setmaxnreg draws on the registers of the launch");
+constexpr int kHtRows = 128, kHtMaxN = 256, kHtK = 64;
+constexpr int kHtBlocks = kHtMaxN / 64;  // blocks of 32 classes a draining warp owns
+// The tensor core cuts off, not rounds, what lies below the accumulator's last place, at every step of 16 inner indices: a sum of 4096 terms
+// came out 2e-6 short.  So a tile's products are summed in chunks of kHtChunk blocks of 64, each in an accumulator of its own, and the chunks
+// are added in registers.
+constexpr int kHtChunk = 12;
+template <bool PAIR> __host__ __device__ constexpr int ht_stages() { return PAIR ? 6 : 4; }
+template <bool PAIR> __host__ __device__ constexpr int ht_stage_bytes() { return (kHtRows + (PAIR ? kHtMaxN / 2 : kHtMaxN)) * kHtK * 2; }
+template <bool PAIR> __host__ __device__ constexpr int ht_smem_bytes() { return ht_stages<PAIR>() * ht_stage_bytes<PAIR>() + 1024 + 256; }
+
+struct HeadTile {
+  int tile_n, run;     // classes of a tile, consecutive tiles of a unit of work
+  int n_tiles, m_tiles, runs;
+  int a_rows;          // rows of h a load brings in (a multiple of 8, at most 128)
+  int w_shared;        // one head for all workers
+  uint32_t idesc;
+  int64_t units;       // K * runs * m_tiles
+};
+
+// The statistics of 32 logits of a row: classes c0 .. c0 + 31, of which `have` exist.  *at_label receives the label's logit.
+__device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int64_t c0, int have, const float* bias, int32_t y, float* at_label) {
+  if (bias != nullptr) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) l[j] += __ldg(bias + c0 + min(j, have - 1));
+  }
+  if (have < 32) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) l[j] = j < have ? l[j] : kMasked;
+  }
+  const int64_t at = (int64_t)y - c0;
+  if (at >= 0 && at < 32 && at < have) {
+    float lab = 0.f;
+    // a select per element in PTX: written as an index, or as anything the compiler can turn into one, it puts the array into local memory
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      asm("{\n.reg .pred p;\nsetp.eq.s32 p, %1, %2;\n@p mov.f32 %0, %3;\n}\n" : "+f"(lab) : "r"((int)at), "r"(j), "f"(l[j]));
+    *at_label = lab;
+  }
+  float mx = st.m;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    l[j] = max_nan(l[j], kMasked);
+    mx = fmaxf(mx, l[j]);
+  }
+  if (mx > st.m) stat_rebase(st, mx);
+  const float B = __fmul_rn(st.m, kLog2e);
+  float s2[2] = {0.f, 0.f}, t2[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const float w = fmaf(l[j], kLog2e, -B), e = ex2(w);
+    s2[j & 1] += e;
+    t2[j & 1] = fmaf(e, w, t2[j & 1]);
+  }
+  st.s += s2[0] + s2[1];
+  st.t += t2[0] + t2[1];
+}
+
+// grid: CTAs (pairs: clusters of 2), each walking units u, u + grid, ...; unit = (run of class tiles, row tile) of a worker, row tile fastest
+template <bool PAIR>
+__global__ void __launch_bounds__(kHtThreads, 1)
+head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_constant__ CUtensorMap map_w, HeadArgs a, HeadTile q) {
+  constexpr int STAGES = ht_stages<PAIR>(), A_BYTES = kHtRows * kHtK * 2;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + STAGES * ht_stage_bytes<PAIR>());
+  uint64_t* empty = full + STAGES;
+  uint64_t* acc_full = empty + STAGES;   // [2]
+  uint64_t* acc_empty = acc_full + 2;    // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert((2 * STAGES + 4) * 8 + 8 <= 256, "barrier area");
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
+  const bool leader = rank == 0u;
+  const int64_t unit = PAIR ? blockIdx.x / 2 : blockIdx.x, units = PAIR ? gridDim.x / 2 : gridDim.x;
+  const int k_blocks = (int)((a.inner + kHtK - 1) / kHtK), chunks = (k_blocks + kHtChunk - 1) / kHtChunk;
+  const int b_rows = PAIR ? q.tile_n / 2 : q.tile_n;  // classes staged by this CTA
+  const uint32_t stage_tx = (uint32_t)(q.a_rows + b_rows) * kHtK * 2;
+
+  grid_dep_launch();
+  if (threadIdx.x == 0) {
+    tc::prefetch_tensormap(&map_h);
+    tc::prefetch_tensormap(&map_w);
+    for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&full[s], 1); tc::mbar_init(&empty[s], 1); }
+    for (int s = 0; s < 2; ++s) { tc::mbar_init(&acc_full[s], 1); tc::mbar_init(&acc_empty[s], PAIR ? 16 : 8); }
+    *abort_flag = 0;
+    tc::fence_barrier_init();
+  }
+  if (warp == 1) {
+    if (PAIR) tc::tmem_alloc_pair(tmem_slot, 512);
+    else tc::tmem_alloc(tmem_slot, 512);
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if (PAIR) tc::cluster_sync_all();
+  tc::tc_fence_after();
+  grid_dep_wait();
+  const uint32_t tmem_base = *tmem_slot;  // 512 columns: the whole tensor memory, so 0 in both CTAs of a pair
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHtRegsIssue));
+    if (warp == 0 && lane == 0) {
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int64_t u = unit; u < q.units && ok; u += units) {
+        const int mt = (int)(u % q.m_tiles), rn = (int)((u / q.m_tiles) % q.runs), k = (int)(u / ((int64_t)q.m_tiles * q.runs));
+        const int r0 = (mt * (PAIR ? 2 : 1) + (int)rank) * kHtRows, kw = q.w_shared ? 0 : k;
+        const int nt_end = min(q.n_tiles, (rn + 1) * q.run);
+        for (int nt = rn * q.run; nt < nt_end && ok; ++nt) {
+          const int c0 = nt * q.tile_n + (int)rank * b_rows;
+          for (int kb = 0; kb < k_blocks; ++kb) {
+            if (!tc::mbar_wait(&empty[s], ph ^ 1u, abort_flag)) { ok = false; break; }
+            uint8_t* dst = ring + s * ht_stage_bytes<PAIR>();
+            if (PAIR) {
+              if (leader) tc::mbar_expect_tx(&full[s], 2 * stage_tx);
+              const uint32_t bar = tc::map_to_cta(tc::smem_u32(&full[s]), 0u);
+              tc::tma_load_3d_pair(dst, &map_h, kb * kHtK, r0, k, bar);
+              tc::tma_load_3d_pair(dst + A_BYTES, &map_w, kb * kHtK, c0, kw, bar);
+            } else {
+              tc::mbar_expect_tx(&full[s], stage_tx);
+              tc::tma_load_3d(dst, &map_h, kb * kHtK, r0, k, &full[s]);
+              tc::tma_load_3d(dst + A_BYTES, &map_w, kb * kHtK, c0, kw, &full[s]);
+            }
+            if (++s == STAGES) { s = 0; ph ^= 1u; }
+          }
+        }
+      }
+      if (!ok) *abort_flag = 1;
+    }
+    if (warp == 1 && lane == 0 && leader) {
+      int s = 0, as = 0;
+      uint32_t ph = 0, aph = 0;
+      bool ok = true;
+      for (int64_t u = unit; u < q.units && ok; u += units) {
+        const int rn = (int)((u / q.m_tiles) % q.runs), nt_end = min(q.n_tiles, (rn + 1) * q.run);
+        for (int nt = rn * q.run; nt < nt_end && ok; ++nt) {
+          for (int kb = 0; kb < k_blocks; ++kb) {
+            const int in_chunk = kb % kHtChunk;
+            if (in_chunk == 0 && !tc::mbar_wait(&acc_empty[as], aph ^ 1u, abort_flag)) { ok = false; break; }
+            const uint32_t d = tmem_base + (uint32_t)as * kHtMaxN;
+            if (!tc::mbar_wait(&full[s], ph, abort_flag)) { ok = false; break; }
+            tc::tc_fence_after();
+            const uint32_t pa = tc::smem_u32(ring + s * ht_stage_bytes<PAIR>()), pb = pa + A_BYTES;
+#pragma unroll
+            for (int k = 0; k < kHtK / 16; ++k) {
+              const uint64_t ad = tc::smem_desc(pa + k * 32, 16, 1024), bd = tc::smem_desc(pb + k * 32, 16, 1024);
+              if (PAIR) tc::umma_bf16_pair(d, ad, bd, q.idesc, (in_chunk | k) != 0 ? 1u : 0u);
+              else tc::umma_bf16(d, ad, bd, q.idesc, (in_chunk | k) != 0 ? 1u : 0u);
+            }
+            if (PAIR) tc::umma_commit_pair(&empty[s]);
+            else tc::umma_commit(&empty[s]);
+            if (++s == STAGES) { s = 0; ph ^= 1u; }
+            if (in_chunk == kHtChunk - 1 || kb == k_blocks - 1) {
+              if (PAIR) tc::umma_commit_pair(&acc_full[as]);
+              else tc::umma_commit(&acc_full[as]);
+              if (++as == 2) { as = 0; aph ^= 1u; }
+            }
+          }
+        }
+      }
+      if (!ok) *abort_flag = 1;
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kHtRegsDrain));
+    const int quad = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t acc_empty_leader[2] = {PAIR ? tc::map_to_cta(tc::smem_u32(&acc_empty[0]), 0u) : 0u, PAIR ? tc::map_to_cta(tc::smem_u32(&acc_empty[1]), 0u) : 0u};
+    int as = 0;
+    uint32_t aph = 0;
+    bool ok = true;
+    for (int64_t u = unit; u < q.units; u += units) {  // every unit, also after giving up: its statistics are then NaN
+      const int mt = (int)(u % q.m_tiles), rn = (int)((u / q.m_tiles) % q.runs), k = (int)(u / ((int64_t)q.m_tiles * q.runs));
+      const int64_t r = (int64_t)(mt * (PAIR ? 2 : 1) + (int)rank) * kHtRows + quad * 32 + lane;
+      const bool live = r < a.rows;
+      const int64_t i = (int64_t)k * a.rows + r;
+      const int32_t y = (live && a.labels) ? a.labels[i] : -1;
+      const float* bias = a.bias ? a.bias + k * a.bk : nullptr;
+      RowStat st = stat_empty();
+      const int nt_end = min(q.n_tiles, (rn + 1) * q.run);
+      for (int nt = rn * q.run; nt < nt_end && ok; ++nt) {
+        const int64_t c_tile = (int64_t)nt * q.tile_n;
+        const int nv = (int)min((int64_t)q.tile_n, a.classes - c_tile);  // classes that exist
+        float l[kHtBlocks][32];  // this warp's blocks of 32 classes: half, half + 2, ...
+        for (int ch = 0; ch < chunks && ok; ++ch) {
+          if (!tc::mbar_wait(&acc_full[as], aph, abort_flag)) { ok = false; break; }
+          tc::tc_fence_after();
+          const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)as * kHtMaxN;
+#pragma unroll
+          for (int b = 0; b < kHtBlocks; ++b) {
+            const int c = (2 * b + half) * 32;
+            if (c < nv) {
+              uint32_t raw[32];
+              tc::tmem_ld32(taddr + (uint32_t)c, raw);
+              tc::tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) l[b][j] = ch == 0 ? __uint_as_float(raw[j]) : l[b][j] + __uint_as_float(raw[j]);
+            }
+          }
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (PAIR) tc::mbar_arrive_cluster(acc_empty_leader[as]);
+            else tc::mbar_arrive(&acc_empty[as]);
+          }
+          if (++as == 2) { as = 0; aph ^= 1u; }
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int b = 0; b < kHtBlocks; ++b) {
+          const int c = (2 * b + half) * 32;
+          if (c < nv) ht_block_stats(l[b], st, c_tile + c, nv - c, bias, y, a.at_label + i);
+        }
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        st = {0.f, NAN, NAN};
+      }
+      if (live) a.part[(int64_t)(rn * 2 + half) * a.total + i] = st;
+    }
+  }
+  __syncwarp();
+  tc::tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {  // copies that may still be in flight land before shared memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) { }
+    __syncthreads();
+  }
+  // neither CTA of a pair leaves while the other can still read its shared memory, write its barriers or fill its tensor memory
+  if (PAIR) tc::cluster_sync_all();
+  tc::tc_fence_after();
+  if (warp == 1) {
+    if (PAIR) tc::tmem_dealloc_pair(tmem_base, 512);
+    else tc::tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+// The width of a tile and the run of tiles that load the machine most evenly: the CTAs (pairs) work through ceil(units / CTAs) rounds of `run`
+// tiles; a tile costs its width plus the share of h it takes in (measured as 32 classes' worth).  Longer runs leave fewer partial statistics.
+// 32768 classes, 4 rows: 147 tiles of 224 instead of 128 of 256, so that every SM streams its share of w.
+inline HeadTile ht_plan(int32_t K, int64_t rows, int64_t classes) {
+  HeadTile q{};
+  const bool pair = rows > kHtRows;
+  const int64_t ctas = pair ? 74 : 148;
+  q.m_tiles = (int)ceil_div(rows, pair ? 2 * kHtRows : kHtRows);
+  double best = 0.0;
+  for (int n = kHtMaxN; n >= 32; n -= 32) {
+    const int64_t n_tiles = ceil_div(classes, (int64_t)n);
+    for (int64_t run = std::min<int64_t>(n_tiles, 32); run >= 1; --run) {
+      const int64_t runs = ceil_div(n_tiles, run);
+      const double cost = (double)ceil_div((int64_t)K * q.m_tiles * runs, ctas) * run * (n + 32) * (1.0 + 0.02 / run);
+      if (best == 0.0 || cost < best) {
+        best = cost;
+        q.tile_n = n; q.run = (int)run; q.n_tiles = (int)n_tiles; q.runs = (int)runs;
+      }
+    }
+  }
+  q.units = (int64_t)K * q.m_tiles * q.runs;
+  q.a_rows = pair ? kHtRows : (int)round_up(rows, 8);
+  return q;
+}
+
+// 16-bit tensor [Z][rows][inner], inner contiguous; boxes of 64 inner indices x box_rows
+template <typename T>
+inline bool ht_make_map(CUtensorMap* m, const T* base, uint64_t inner, uint64_t rows, uint64_t Z, int64_t row_stride, int64_t z_stride, uint32_t box_rows) {
+  PFN_encodeTiled enc = tc_encode_fn();
+  if (!enc) return false;
+  // the stride of a dimension of one element is never used, but has to be a legal one
+  const uint64_t rs = rows > 1 ? (uint64_t)row_stride * 2 : (uint64_t)round_up((int64_t)inner * 2, 16);
+  const uint64_t zs = Z > 1 ? (uint64_t)z_stride * 2 : rs;
+  if ((reinterpret_cast<uintptr_t>(base) & 15) || rs % 16 || zs % 16 || rs == 0 || zs == 0 || rs >= ((uint64_t)1 << 40) || zs >= ((uint64_t)1 << 40)) return false;
+  cuuint64_t dims[3] = {inner, rows, Z};
+  cuuint64_t strides[2] = {rs, zs};
+  cuuint32_t box[3] = {(cuuint32_t)kHtK, box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(m, std::is_same<T, bf16>::value ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<T*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// False (nothing launched): the operands' addresses or strides are not what TMA takes.  *e: the launch's error.
+template <typename T>
+inline bool ht_launch(const T* h, const T* w, HeadArgs a, int32_t K, HeadTile q, cudaStream_t stream, cudaError_t* e) {
+  const bool pair = a.rows > kHtRows;
+  CUtensorMap mh, mw;
+  q.w_shared = a.wk == 0 || K == 1;
+  if (!ht_make_map(&mh, h, a.inner, a.rows, K, a.hr, a.hk, (uint32_t)q.a_rows)) return false;
+  if (!ht_make_map(&mw, w, a.inner, a.classes, q.w_shared ? 1 : K, a.wr, a.wk, (uint32_t)(pair ? q.tile_n / 2 : q.tile_n))) return false;
+  q.idesc = tc::instr_desc(pair ? 256 : 128, q.tile_n, false, false);
+  if (!std::is_same<T, bf16>::value) q.idesc &= ~((1u << 7) | (1u << 10));  // operands f16 instead of bf16
+  a.parts = 2 * q.runs;
+  const void* kern = pair ? (const void*)head_tcgen05_kernel<true> : (const void*)head_tcgen05_kernel<false>;
+  const int smem = pair ? ht_smem_bytes<true>() : ht_smem_bytes<false>();
+  if ((*e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return true;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(pair ? 2 * std::min<int64_t>(q.units, 74) : std::min<int64_t>(q.units, 148)));
+  cfg.blockDim = dim3(kHtThreads); cfg.dynamicSmemBytes = smem; cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = pair ? 1 : 0;
+  void* args[] = {&mh, &mw, &a, &q};
+  *e = cudaLaunchKernelExC(&cfg, kern, args);
+  return true;
+}
+
+}  // namespace lsam

@@ -10,6 +10,7 @@
 #include "dropout.cuh"
 #include "head_ops.cuh"
 #include "head_score.cuh"
+#include "head_tcgen05.cuh"
 
 using namespace lsam;
 
@@ -139,26 +140,30 @@ extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K,
 
 namespace {
 
-// How a head call is cut: enough shares of the classes to occupy the machine, none shorter than a few tiles.
-struct HeadPlan {
+// SIMT form of a head call: enough shares of the classes to occupy the machine, none shorter than a tile.
+struct SimtPlan {
   int splits = 1;
   int64_t per_split = 0;
 };
-HeadPlan head_plan(int32_t K, int64_t rows, int64_t classes) {
-  HeadPlan p;
+SimtPlan simt_plan(int32_t K, int64_t rows, int64_t classes) {
+  SimtPlan p;
   const int64_t blocks = (int64_t)K * ceil_div(rows, kHsM);
-  int64_t splits = std::min<int64_t>(ceil_div(2 * 148, blocks), ceil_div(classes, kHsN));
-  p.per_split = round_up(ceil_div(classes, std::max<int64_t>(splits, 1)), kHsN);
+  const int64_t splits = std::min<int64_t>(ceil_div(2 * 148, blocks), ceil_div(classes, kHsN));
+  p.per_split = round_up(ceil_div(classes, splits), kHsN);
   p.splits = (int)ceil_div(classes, p.per_split);
   return p;
 }
-size_t head_bytes(const HeadPlan& p, int64_t total) { return (size_t)round_up((int64_t)sizeof(RowStat) * p.splits * total, 256) + 4 * (size_t)total; }
+// partial statistics of either form, then the labels' logits
+size_t head_part_bytes(int32_t K, int64_t rows, int64_t classes) {
+  const int64_t parts = std::max<int64_t>(simt_plan(K, rows, classes).splits, 2 * ht_plan(K, rows, classes).runs);
+  return (size_t)round_up((int64_t)sizeof(RowStat) * parts * K * rows, 256);
+}
 
 }  // namespace
 
 extern "C" size_t lsam_head_logprob_workspace_bytes(int32_t K, int64_t rows, int64_t classes) {
   if (K < 1 || rows < 1 || classes < 1 || rows > kMaxIndex / K || classes > kMaxIndex) return 0;
-  return head_bytes(head_plan(K, rows, classes), (int64_t)K * rows);
+  return head_part_bytes(K, rows, classes) + 4 * (size_t)K * rows;
 }
 
 extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
@@ -174,25 +179,47 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
   if (K > 65535 || rows > kMaxIndex / K || rows > (int64_t)kHsM * 65535) return err.fail(LSAM_ERR_INVALID, "need K <= 65535, rows <= 4194240, K * rows < 2^31");
   if (!strides_ok(K, h_stride_k, rows, h_stride_row, inner, 1) || !strides_ok(K, w_stride_k, classes, w_stride_class, inner, 1) || bias_stride_k < 0)
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
-  const HeadPlan plan = head_plan(K, rows, classes);
   const int64_t total = (int64_t)K * rows;
-  if (workspace_bytes < head_bytes(plan, total)) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_head_logprob_workspace_bytes()");
+  const size_t part_bytes = head_part_bytes(K, rows, classes);
+  if (workspace_bytes < part_bytes + 4 * (size_t)total) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_head_logprob_workspace_bytes()");
   if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return err.fail(LSAM_ERR_WORKSPACE, "workspace not 256-byte aligned");
   PtrCheck pc;
   pc.need(d_h, dtype_size(dtype)); pc.need(d_w, dtype_size(dtype)); pc.need(d_workspace, 256);
   pc.optional(d_bias, 4); pc.optional(d_labels, 4); pc.optional(d_logp, 4); pc.optional(d_lse, 4); pc.optional(d_entropy, 4);
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
-  HeadArgs a{rows, inner, classes, h_stride_k, h_stride_row, w_stride_k, w_stride_class, bias_stride_k, d_bias, d_labels, plan.splits, plan.per_split,
-             static_cast<RowStat*>(d_workspace),
-             reinterpret_cast<float*>(static_cast<char*>(d_workspace) + round_up((int64_t)sizeof(RowStat) * plan.splits * total, 256))};
+  HeadArgs a{rows, inner, classes, total, h_stride_k, h_stride_row, w_stride_k, w_stride_class, bias_stride_k, d_bias, d_labels, 0, 0,
+             static_cast<RowStat*>(d_workspace), reinterpret_cast<float*>(static_cast<char*>(d_workspace) + part_bytes)};
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    head_score_simt_kernel<T><<<dim3((unsigned)plan.splits, (unsigned)ceil_div(rows, kHsM), (unsigned)K), 256, 0, stream>>>(static_cast<const T*>(d_h), static_cast<const T*>(d_w), a);
+    const T *h = static_cast<const T*>(d_h), *w = static_cast<const T*>(d_w);
+    if constexpr (sizeof(T) == 2) {
+      const HeadTile q = ht_plan(K, rows, classes);
+      a.parts = 2 * q.runs;
+      if (ht_launch(h, w, a, K, q, stream, &e)) return;
+    }
+    const SimtPlan p = simt_plan(K, rows, classes);
+    a.parts = p.splits;
+    a.per_split = p.per_split;
+    head_score_simt_kernel<T><<<dim3((unsigned)p.splits, (unsigned)ceil_div(rows, kHsM), (unsigned)K), 256, 0, stream>>>(h, w, a);
+    e = cudaPeekAtLastError();
   });
-  const ScoreOut out{d_logp, d_lse, d_entropy, nullptr, nullptr, 0};
-  head_join_kernel<<<(unsigned)ceil_div(total, 128), 128, 0, stream>>>(a, total, out);
-  return err.launched();
+  if (e == cudaSuccess) {
+    // programmatic dependent launch: the join's blocks become resident while the tiles drain and wait for them there
+    const ScoreOut out{d_logp, d_lse, d_entropy, nullptr, nullptr, 0};
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)ceil_div(total, 32)); cfg.blockDim = dim3(32, 32); cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, head_join_kernel, a, total, out);
+  }
+  if (e != cudaSuccess) {
+    (void)cudaGetLastError();
+    return err.fail(LSAM_ERR_CUDA, cudaGetErrorString(e));
+  }
+  return LSAM_OK;
 }
 
 extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, int32_t dtype, int32_t K, int64_t rows, int64_t n, int64_t x_stride_k,

@@ -34,6 +34,7 @@ def reference(l, labels, top_k):
     """Scores in 64 bits of the stored values, and the bounds of their errors."""
     C = l.shape[-1]
     d = l.double()
+    d = torch.where(d < -1e30, torch.full_like(d, NINF), d)  # masks
     m = torch.where(torch.isnan(d), torch.full_like(d, NINF), d).amax(-1, keepdim=True)
     base = torch.where(torch.isneginf(m), torch.zeros_like(m), m)
     z = (d - base).exp().sum(-1, keepdim=True).log()  # a +inf logit makes it NaN
@@ -189,7 +190,7 @@ def grad_reference(l, y, lse, ent, a, b):
         xe = torch.where(p > 0, x + ent.double().unsqueeze(-1), torch.zeros_like(x))
         g = g - b.double().unsqueeze(-1) * p * xe
         err = err + b.double().abs().unsqueeze(-1) * p * (xe.abs() * (rel + 2 * U) + 3 * U * (torch.where(p > 0, x.abs(), torch.zeros_like(x)) + ent.double().abs().unsqueeze(-1)))
-    none = lse < -1e30  # nothing but masks
+    none = torch.isneginf(lse)  # nothing but masks
     none = none if y is None else none | (y < 0)
     g = torch.where(none.unsqueeze(-1), torch.zeros_like(g), g)
     if y is not None:
@@ -274,6 +275,7 @@ def head_reference(h, w, bias, y):
     mag = h.double().abs() @ w.double().abs().transpose(-1, -2)
     if bias is not None:
         l = l + (bias.double().unsqueeze(-2) if bias.dim() == 2 else bias.double())
+    l = torch.where(l < -1e30, torch.full_like(l, NINF), l)
     # fp32 accumulation, in the tensor cores with truncated addends: at most one step of the running magnitude per term
     l_err = (2 * U * (h.shape[-1] + 8) * mag).amax(-1)
     out = reference(l, y, 0)
