@@ -2,6 +2,8 @@
 // of every row of logits, and the gradient of a loss of the first and the third with respect to the logits.
 #pragma once
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace lsam {
@@ -95,60 +97,472 @@ __device__ inline void write_no_top(const ScoreOut& o, int64_t i, int from) {
   }
 }
 
-// One block per row: a strided pass for the statistics, then one pass per alternative (the best key below the previous one).
-template <typename T>
-__global__ void __launch_bounds__(256)
-logprob_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o) {
-  __shared__ RowStat ws[8];
-  __shared__ uint64_t wk[8];
-  const int64_t i = blockIdx.x;
-  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
-  const int32_t y = labels ? labels[i] : 0;
-  if (y < 0) {
-    if (tid == 0) {
-      if (o.logp) o.logp[i] = 0.f;
-      if (o.lse) o.lse[i] = 0.f;
-      if (o.entropy) o.entropy[i] = 0.f;
-      write_no_top(o, i, 0);
+// ---- 16-byte vectors of logits
+template <typename T> __host__ __device__ constexpr int vec_n() { return 16 / (int)sizeof(T); }
+template <typename T> __device__ inline void vec_unpack(const uint4& q, float (&f)[16 / sizeof(T)]);
+template <> __device__ inline void vec_unpack<float>(const uint4& q, float (&f)[4]) {
+  f[0] = __uint_as_float(q.x); f[1] = __uint_as_float(q.y); f[2] = __uint_as_float(q.z); f[3] = __uint_as_float(q.w);
+}
+template <> __device__ inline void vec_unpack<bf16>(const uint4& q, float (&f)[8]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { f[2 * j] = __uint_as_float(w[j] << 16); f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+}
+template <> __device__ inline void vec_unpack<fp16>(const uint4& q, float (&f)[8]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+    f[2 * j] = p.x; f[2 * j + 1] = p.y;
+  }
+}
+// two fp32 operations per instruction
+__device__ inline uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ inline void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ inline uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ inline uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// Statistics of N logits that are already cut at kMasked, mx their maximum (NaN ignored).
+template <int N>
+__device__ inline void stat_add_all(RowStat& a, const float (&l)[N], float mx) {
+  static_assert(N % 2 == 0, "pairs");
+  if (mx > a.m) stat_rebase(a, mx);
+  const float nb = -__fmul_rn(a.m, kLog2e);
+  const uint64_t k2 = pack2(kLog2e, kLog2e), nb2 = pack2(nb, nb);
+  uint64_t s2 = 0, t2 = 0;
+#pragma unroll
+  for (int j = 0; j < N; j += 2) {
+    const uint64_t w2 = fma2(pack2(l[j], l[j + 1]), k2, nb2);
+    float w0, w1;
+    unpack2(w2, w0, w1);
+    const uint64_t e2 = pack2(ex2(w0), ex2(w1));
+    s2 = add2(s2, e2);
+    t2 = fma2(e2, w2, t2);
+  }
+  float x, y;
+  unpack2(s2, x, y);
+  a.s += x + y;
+  unpack2(t2, x, y);
+  a.t += x + y;
+}
+// Cuts U vectors at kMasked, takes their maximum and adds them.
+template <typename T, int U>
+__device__ inline void stat_add_vecs(RowStat& a, uint4 (&q)[U]) {
+  constexpr int N = vec_n<T>();
+  float mx = kMasked, l[U * N];
+  if constexpr (std::is_same<T, bf16>::value) {
+    // bf16: cut and compared in pairs; the bound is the bf16 next below kMasked
+    constexpr uint32_t cut = 0xf14af14au;
+    uint32_t m2 = cut;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w[j]) : "r"(w[j]), "r"(cut));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(m2) : "r"(m2), "r"(w[j]));
+        l[u * 8 + 2 * j] = __uint_as_float(w[j] << 16);
+        l[u * 8 + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+      }
     }
+    mx = fmaxf(mx, fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xffff0000u)));
+  } else {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[N];
+      vec_unpack<T>(q[u], f);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        l[u * N + j] = max_nan(f[j], kMasked);
+        mx = fmaxf(mx, l[u * N + j]);
+      }
+    }
+  }
+  stat_add_all(a, l, mx);
+}
+
+__device__ inline void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <typename V>
+__device__ inline const V* cluster_map(const V* p, uint32_t rank) {  // the same shared variable of another block of the cluster
+  uint64_t r;
+  asm("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+  return reinterpret_cast<const V*>(r);
+}
+
+// Which elements of a row a thread owns.  The row is [head scalars][16-byte vectors][tail scalars]; thread g of G owns scalars and vectors
+// g, g + G, ... of each part.  A row without unit stride is all head.
+template <typename T>
+struct RowParts {
+  const T* row;
+  int64_t sc;
+  int32_t head, nvec, tail0, classes;
+  __device__ inline RowParts(const T* r, int64_t stride, int32_t C) : row(r), sc(stride), classes(C) {
+    if (stride != 1) { head = C; nvec = 0; tail0 = C; return; }
+    const int32_t off = (int32_t)((16 - (reinterpret_cast<uintptr_t>(r) & 15)) & 15) / (int32_t)sizeof(T);
+    head = off < C ? off : C;
+    nvec = (C - head) / vec_n<T>();
+    tail0 = head + nvec * vec_n<T>();
+  }
+  __device__ inline float at(int64_t c) const { return to_float(row[c * sc]); }
+  __device__ inline uint4 vec(int32_t v) const { return __ldg(reinterpret_cast<const uint4*>(row + head) + v); }
+  // f(value, class) for every element that thread g of G owns; the warp's lanes take its vectors in turn
+  template <class F>
+  __device__ inline void each_of(int g, int G, int lane, F&& f) const {
+    for (int64_t c = g + (int64_t)lane * G; c < head; c += 32 * (int64_t)G) f(at(c), (int32_t)c);
+    for (int64_t v = g + (int64_t)lane * G; v < nvec; v += 32 * (int64_t)G) {
+      const uint4 q = vec((int32_t)v);
+      float l[vec_n<T>()];
+      vec_unpack<T>(q, l);
+#pragma unroll
+      for (int j = 0; j < vec_n<T>(); ++j) f(l[j], head + (int32_t)v * vec_n<T>() + j);
+    }
+    const int64_t c = (int64_t)tail0 + g;  // the tail is shorter than a vector
+    if (lane == 0 && c < classes) f(at(c), (int32_t)c);
+  }
+};
+
+// k-th largest (k <= 32) of the values of a warp's lanes: the least value that fewer than k others exceed
+__device__ inline float warp_kth(float v, int k) {
+  int above = 0;
+#pragma unroll
+  for (int d = 1; d < 32; ++d) above += __shfl_xor_sync(~0u, v, d) > v;
+  float t = above < k ? v : INFINITY;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) t = fminf(t, __shfl_xor_sync(~0u, t, d));
+  return t;
+}
+
+template <int NT> __host__ __device__ constexpr int top_list() { return NT > 32 ? 512 : 128; }  // candidates a block keeps
+template <int NT>
+struct TopShared {
+  float kth[(NT + 31) / 32];
+  float maxima[NT];
+  int owners[NT];
+  uint64_t above[top_list<NT>()], equal[top_list<NT>()];  // keys of elements above / at the threshold
+  uint64_t best[kTopMax];
+  int n_max, n_own, n_above, n_equal;
+  uint32_t thr;
+};
+
+// The k best keys of the elements that the NT threads of a block own -> sh.best in order (0: none), valid after the call.  vm = the
+// caller's own maximum (cut at kMasked, NaN ignored).  At least k threads have a maximum >= T, T the k-th largest of the maxima, so the k
+// best elements are >= T and belong to those threads: only their elements are read again (from L2), and what passes T is ranked by
+// counting.  T is found in two steps, the largest of the warps' own k-th values, then exactly among the maxima that pass it.
+//   More than top_list elements at T (tied rows): the lowest classes are picked in order by one warp, which stops at the k-th.
+//   More than top_list above T: k passes over the block's elements.
+template <typename T, int NT>
+__device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, int k, TopShared<NT>& sh) {
+  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+  constexpr int NW = (NT + 31) / 32, LIST = top_list<NT>();
+  const float kw = warp_kth(vm, k);
+  if (lane == 0) sh.kth[w] = kw;
+  if (tid == 0) { sh.n_max = sh.n_own = sh.n_above = sh.n_equal = 0; sh.thr = 0xffffffffu; }
+  if (tid < kTopMax) sh.best[tid] = 0;
+  __syncthreads();
+  float thr = sh.kth[0];
+#pragma unroll
+  for (int q = 1; q < NW; ++q) thr = fmaxf(thr, sh.kth[q]);
+  if (NW > 1) {
+    const bool in = vm >= thr;
+    if (in) sh.maxima[atomicAdd(&sh.n_max, 1)] = vm;
+    __syncthreads();
+    if (in) {
+      int above = 0;
+      for (int q = 0; q < sh.n_max; ++q) above += sh.maxima[q] > vm;
+      if (above < k) atomicMin(&sh.thr, order_bits(vm));
+    }
+    __syncthreads();
+    thr = order_value(sh.thr);
+  }
+  if (vm >= thr) sh.owners[atomicAdd(&sh.n_own, 1)] = tid;
+  __syncthreads();
+  for (int q = w; q < sh.n_own; q += NW)
+    rp.each_of(g0 + sh.owners[q], G, lane, [&](float l, int32_t c) {
+      if (l > thr) {
+        const int at = atomicAdd(&sh.n_above, 1);
+        if (at < LIST) sh.above[at] = order_key(l, c);
+      } else if (l == thr) {
+        const int at = atomicAdd(&sh.n_equal, 1);
+        if (at < LIST) sh.equal[at] = order_key(l, c);
+      }
+    });
+  __syncthreads();
+  const int na = sh.n_above, ne = sh.n_equal;
+  if (na > LIST) {
+    uint64_t last = ~0ull;
+    for (int j = 0; j < k; ++j) {
+      uint64_t best = 0;
+      auto see = [&](float l, int32_t c) {
+        const uint64_t key = order_key(l, c);
+        if (key < last && key > best) best = key;
+      };
+      for (int q = w; q < sh.n_own; q += NW) rp.each_of(g0 + sh.owners[q], G, lane, see);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) best = max(best, (uint64_t)__shfl_xor_sync(~0u, (unsigned long long)best, d));
+      __syncthreads();
+      if (lane == 0) sh.equal[w] = best;
+      __syncthreads();
+      for (int q = 0; q < NW; ++q) best = max(best, sh.equal[q]);
+      if (tid == 0) sh.best[j] = best;
+      last = best;  // 0: nothing is left
+    }
+    __syncthreads();
     return;
   }
-  const T* row = v.row(i);
-  RowStat a = stat_empty();
-  for (int c = tid; c < v.classes; c += 256) stat_add(a, to_float(row[c * v.sc]));
-  for (int d = 16; d > 0; d >>= 1) a = stat_merge(a, stat_shfl_xor(a, d));
-  if (lane == 0) ws[w] = a;
+  for (int q = tid; q < na; q += NT) {
+    const uint64_t key = sh.above[q];
+    int r = 0;
+    for (int p = 0; p < na; ++p) r += sh.above[p] > key;
+    if (r < k) sh.best[r] = key;
+  }
+  if (na < k && ne <= LIST) {
+    for (int q = tid; q < ne; q += NT) {
+      const uint64_t key = sh.equal[q];
+      int r = na;
+      for (int p = 0; p < ne; ++p) r += sh.equal[p] > key;
+      if (r < k) sh.best[r] = key;
+    }
+  } else if (na < k && w == 0) {
+    int have = na;  // the lowest classes at T, in order
+    auto take = [&](uint32_t mask, int32_t c0) {  // this lane's elements c0 + bit, lanes ascending
+      int incl = __popc(mask);
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(~0u, incl, d);
+        if (lane >= d) incl += o;
+      }
+      int at = have + incl - __popc(mask);
+      for (; mask && at < k; mask &= mask - 1) sh.best[at++] = order_key(thr, c0 + __ffs(mask) - 1);
+      have += __shfl_sync(~0u, incl, 31);
+    };
+    for (int64_t j = 0; j < rp.head && have < k; j += G)
+      for (int t = 0; t < NT && have < k; t += 32) {
+        const int64_t c = j + g0 + t + lane;
+        take(c < rp.head && rp.at(c) == thr, (int32_t)c);
+      }
+    for (int64_t j = 0; j < rp.nvec && have < k; j += G)
+      for (int t = 0; t < NT && have < k; t += 32) {
+        const int64_t v = j + g0 + t + lane;
+        uint32_t mask = 0;
+        if (v < rp.nvec) {
+          float l[vec_n<T>()];
+          vec_unpack<T>(rp.vec((int32_t)v), l);
+#pragma unroll
+          for (int e = 0; e < vec_n<T>(); ++e) mask |= (l[e] == thr ? 1u : 0u) << e;
+        }
+        take(mask, rp.head + (int32_t)v * vec_n<T>());
+      }
+    const int64_t c = (int64_t)rp.tail0 + g0 + lane;  // the tail is shorter than a vector
+    if (have < k) take(c < rp.classes && rp.at(c) == thr, (int32_t)c);
+  }
   __syncthreads();
-  a = ws[0];
-  for (int q = 1; q < 8; ++q) a = stat_merge(a, ws[q]);
+}
+
+__device__ inline void write_left_out(const ScoreOut& o, int64_t i) {
+  if (o.logp) o.logp[i] = 0.f;
+  if (o.lse) o.lse[i] = 0.f;
+  if (o.entropy) o.entropy[i] = 0.f;
+  write_no_top(o, i, 0);
+}
+template <typename L>
+__device__ inline void write_scores(const ScoreOut& o, int64_t i, const RowScore& sc, int32_t y, int32_t classes, L&& label_logit) {
+  if (o.logp) o.logp[i] = y < classes ? score_logp(label_logit(), sc) : NAN;
+  if (o.lse) o.lse[i] = sc.lse;
+  if (o.entropy) o.entropy[i] = sc.ent;
+}
+__device__ inline void write_top(const ScoreOut& o, int64_t i, int j, uint64_t key, const RowScore& sc) {
+  o.top_logp[i * o.top_k + j] = key ? score_logp(order_value((uint32_t)(key >> 32)), sc) : -INFINITY;
+  o.top_idx[i * o.top_k + j] = key ? (int32_t)~(uint32_t)key : -1;
+}
+
+// Rows of contiguous classes: NT threads of CS blocks (a cluster) per row, one pass.  A thread keeps the statistics of the vectors it owns in
+// registers, four (fp32: eight) vectors per step so that 64 (128) bytes a thread are in flight; nothing is exchanged until the row ends.
+template <typename T, int NT, int CS>
+__global__ void __launch_bounds__(NT)
+logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o) {
+  constexpr int NW = NT / 32, U = 4 * (int)sizeof(T) / 2, G = NT * CS;
+  __shared__ RowStat ws[NW], cta;
+  __shared__ TopShared<NT> sh;
+  const int64_t i = blockIdx.x / CS;
+  const int part = CS > 1 ? (int)(blockIdx.x % CS) : 0;
+  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g0 = part * NT, g = g0 + tid;
+  const int32_t y = labels ? labels[i] : 0;
+  if (y < 0) {  // the same for every block of the cluster
+    if (g == 0) write_left_out(o, i);
+    return;
+  }
+  const RowParts<T> rp(v.row(i), v.sc, v.classes);
+  RowStat a = stat_empty();
+  for (int64_t c = g; c < rp.head; c += G) stat_add(a, rp.at(c));
+  if ((int64_t)rp.tail0 + g < rp.classes) stat_add(a, rp.at(rp.tail0 + g));
+  int64_t q = g;
+  for (; q + (U - 1) * G < rp.nvec; q += U * G) {
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = rp.vec((int32_t)q + u * G);
+    stat_add_vecs<T, U>(a, x);
+  }
+  for (; q < rp.nvec; q += G) {
+    uint4 x[1] = {rp.vec((int32_t)q)};
+    stat_add_vecs<T, 1>(a, x);
+  }
+  const float vm = a.m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) a = stat_merge(a, stat_shfl_xor(a, d));
+  if (NW > 1) {
+    if (lane == 0) ws[w] = a;
+    __syncthreads();
+    a = ws[0];
+#pragma unroll
+    for (int p = 1; p < NW; ++p) a = stat_merge(a, ws[p]);
+  }
+  if (o.top_k > 0) block_top<T, NT>(rp, g0, G, vm, o.top_k, sh);
+  if (CS > 1) {
+    if (tid == 0) cta = a;
+    cluster_sync();
+    if (part == 0) {
+      a = cta;
+#pragma unroll
+      for (int p = 1; p < CS; ++p) a = stat_merge(a, *cluster_map(&cta, p));
+      if (o.top_k > 0) {
+        // rank the CS * k keys of the blocks: all into this block's list first
+        const int n = CS * o.top_k;
+        for (int p = tid; p < n; p += NT) sh.above[p] = cluster_map(sh.best, p / o.top_k)[p % o.top_k];
+        __syncthreads();
+        if (tid < kTopMax) sh.equal[tid] = 0;
+        __syncthreads();
+        for (int p = tid; p < n; p += NT) {
+          const uint64_t key = sh.above[p];
+          int r = 0;
+          for (int z = 0; z < n; ++z) r += sh.above[z] > key;
+          if (key && r < o.top_k) sh.equal[r] = key;
+        }
+        __syncthreads();
+      }
+    }
+    cluster_sync();  // no block leaves while its shared memory is read
+    if (part != 0) return;
+  }
   const RowScore sc = stat_finish(a);
-  if (tid == 0) {
-    if (o.logp) o.logp[i] = y < v.classes ? score_logp(to_float(row[y * v.sc]), sc) : NAN;
-    if (o.lse) o.lse[i] = sc.lse;
-    if (o.entropy) o.entropy[i] = sc.ent;
+  if (tid == 0) write_scores(o, i, sc, y, v.classes, [&] { return rp.at(y); });
+  if (tid < o.top_k) write_top(o, i, tid, CS > 1 ? sh.equal[tid] : sh.best[tid], sc);
+}
+
+// Logits with the sample index contiguous: 16 rows x 32 groups of classes per block, group y owns classes y, y + 32, ...; a warp reads two runs
+// of 16 consecutive samples.  A chunk of 32 x kFeatN classes is loaded into registers in one go, and stays there for the alternatives when it is the whole row.
+constexpr int kFeatR = 16, kFeatG = 32, kFeatN = 32, kFeatList = 48;
+template <typename T>
+__global__ void __launch_bounds__(kFeatR * kFeatG)
+logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o, int row_blocks) {
+  __shared__ float red[3][kFeatR][kFeatG + 1];
+  __shared__ uint64_t list[kFeatR][kFeatList];
+  __shared__ uint64_t best[kFeatR][kTopMax];
+  __shared__ float thr_s[kFeatR];
+  __shared__ int count[kFeatR];
+  const int x = threadIdx.x % kFeatR, y = threadIdx.x / kFeatR;
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t k = blockIdx.x / row_blocks, r0 = (int64_t)(blockIdx.x % row_blocks) * kFeatR, r = r0 + x, i = k * v.rows + r;
+  const bool in = r < v.rows;
+  const int32_t lab = in && labels ? labels[i] : 0;
+  const bool live = in && lab >= 0;
+  const T* p = v.p + k * v.sk + (live ? r : 0) * v.sr;
+  RowStat a = stat_empty();
+  float l[kFeatN];
+  for (int64_t c0 = 0; c0 < v.classes; c0 += kFeatG * kFeatN) {
+    float mx = kMasked;
+#pragma unroll
+    for (int j = 0; j < kFeatN; ++j) {
+      const int64_t c = c0 + y + kFeatG * j;
+      l[j] = live && c < v.classes ? to_float(p[c * v.sc]) : -INFINITY;
+    }
+    float m[kFeatN];  // l itself keeps the masks' own values for the alternatives
+#pragma unroll
+    for (int j = 0; j < kFeatN; ++j) {
+      m[j] = max_nan(l[j], kMasked);
+      mx = fmaxf(mx, m[j]);
+    }
+    stat_add_all(a, m, mx);
   }
-  uint64_t last = ~0ull;
-  for (int j = 0; j < o.top_k; ++j) {
-    uint64_t best = 0;
-    for (int c = tid; c < v.classes; c += 256) {
-      const uint64_t k = order_key(to_float(row[c * v.sc]), c);
-      if (k < last && k > best) best = k;
-    }
-    for (int d = 16; d > 0; d >>= 1) best = max(best, (uint64_t)__shfl_xor_sync(~0u, (unsigned long long)best, d));
-    __syncthreads();
-    if (lane == 0) wk[w] = best;
-    __syncthreads();
-    for (int q = 0; q < 8; ++q) best = max(best, wk[q]);
-    if (best == 0) {
-      if (tid == 0) write_no_top(o, i, j);
-      break;
-    }
-    if (tid == 0) {
-      o.top_logp[i * o.top_k + j] = score_logp(order_value((uint32_t)(best >> 32)), sc);
-      o.top_idx[i * o.top_k + j] = (int32_t)~(uint32_t)best;
-    }
-    last = best;
+  const float vm = a.m;
+  red[0][x][y] = a.m; red[1][x][y] = a.s; red[2][x][y] = a.t;
+  if (threadIdx.x < kFeatR) count[threadIdx.x] = 0;
+  __syncthreads();
+  // warp w joins row w over its 32 groups; the threshold of the row is the k-th largest of the groups' maxima
+  a = {red[0][w][lane], red[1][w][lane], red[2][w][lane]};
+  if (o.top_k > 0) {
+    const float t = warp_kth(a.m, o.top_k);
+    if (lane == 0) thr_s[w] = t;
+    best[w][lane] = 0;
   }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) a = stat_merge(a, stat_shfl_xor(a, d));
+  const RowScore sc = stat_finish(a);
+  const int64_t rw = r0 + w, iw = k * v.rows + rw;
+  const bool row_in = rw < v.rows;
+  const int32_t yw = row_in && labels ? labels[iw] : 0;
+  const T* pw = v.p + k * v.sk + (row_in ? rw : 0) * v.sr;
+  if (lane == 0 && row_in) {
+    if (yw < 0) write_left_out(o, iw);
+    else write_scores(o, iw, sc, yw, v.classes, [&] { return to_float(pw[(int64_t)yw * v.sc]); });
+  }
+  if (o.top_k == 0) return;
+  __syncthreads();
+  const float thr = thr_s[x];
+  auto offer = [&](float val, int64_t c) {
+    if (val >= thr && val >= kMasked) {
+      const int at = atomicAdd(&count[x], 1);
+      if (at < kFeatList) list[x][at] = order_key(val, (int32_t)c);
+    }
+  };
+  if (live && vm >= thr) {
+    if (v.classes <= kFeatG * kFeatN) {
+#pragma unroll
+      for (int j = 0; j < kFeatN; ++j) offer(l[j], y + kFeatG * j);
+    } else {
+      for (int64_t c = y; c < v.classes; c += kFeatG) offer(to_float(p[c * v.sc]), c);
+    }
+  }
+  __syncthreads();
+  if (!row_in || yw < 0) return;
+  const int n = count[w];
+  if (n <= kFeatList) {
+    for (int q = lane; q < n; q += 32) {
+      const uint64_t key = list[w][q];
+      int rank = 0;
+      for (int z = 0; z < n; ++z) rank += list[w][z] > key;
+      if (rank < o.top_k) best[w][rank] = key;
+    }
+  } else {
+    // more candidates than the list holds (ties): one pass of the warp per alternative
+    uint64_t last = ~0ull;
+    for (int j = 0; j < o.top_k; ++j) {
+      uint64_t b = 0;
+      for (int64_t c = lane; c < v.classes; c += 32) {
+        const uint64_t key = order_key(to_float(pw[c * v.sc]), (int32_t)c);
+        if (key < last && key > b) b = key;
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) b = max(b, (uint64_t)__shfl_xor_sync(~0u, (unsigned long long)b, d));
+      if (lane == 0) best[w][j] = b;
+      last = b;
+    }
+  }
+  __syncwarp();
+  if (lane < o.top_k) write_top(o, iw, lane, best[w][lane], sc);
 }
 
 // Gradient of L(logp, entropy) of every row:  dl_c = a (1[c = y] - p_c) - b p_c (log p_c + H),  p_c = e^(l_c - lse),

@@ -27,9 +27,9 @@ struct Err {
     if (buf && len > 0) std::snprintf(buf, len, "%s: %s", fn, msg);
     return code;
   }
-  int launched() const {
-    const cudaError_t e = cudaGetLastError();
+  int done(cudaError_t e) const {
     if (e == cudaSuccess) return LSAM_OK;
+    (void)cudaGetLastError();
     if (buf && len > 0) std::snprintf(buf, len, "%s: launch failed: %s", fn, cudaGetErrorString(e));
     return LSAM_ERR_CUDA;
   }
@@ -79,6 +79,38 @@ void by_dtype(int32_t d, F&& f) {
 
 }  // namespace
 
+namespace {
+
+template <typename T, int NT, int CS>
+cudaError_t launch_row(const LogitView<T>& v, const int32_t* labels, const ScoreOut& out, int64_t total, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(total * CS)); cfg.blockDim = dim3(NT); cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = CS > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, logprob_row_kernel<T, NT, CS>, v, labels, out);
+}
+
+// Which form a call takes.  Sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 2 KB, 128 threads up
+// to 16 KB, else 256; rows that do not fill the machine are split over a cluster of 2 or 8 blocks while every thread keeps two vectors.
+template <typename T>
+cudaError_t launch_scores(const LogitView<T>& v, const int32_t* labels, const ScoreOut& out, int32_t K, cudaStream_t stream) {
+  const int64_t total = (int64_t)K * v.rows;
+  if (v.sc != 1 && v.sr == 1 && v.rows > 1) {
+    const int64_t row_blocks = ceil_div(v.rows, kFeatR);
+    logprob_feature_kernel<T><<<(unsigned)(K * row_blocks), kFeatR * kFeatG, 0, stream>>>(v, labels, out, (int)row_blocks);
+    return cudaPeekAtLastError();
+  }
+  const int64_t bytes = (int64_t)v.classes * sizeof(T);
+  if (bytes <= 2048) return launch_row<T, 32, 1>(v, labels, out, total, stream);
+  if (bytes <= 16384 && total >= 148) return launch_row<T, 128, 1>(v, labels, out, total, stream);
+  if (total >= 2 * 148 || bytes < 16384) return launch_row<T, 256, 1>(v, labels, out, total, stream);
+  if (total >= 148 / 2 || bytes < 65536) return launch_row<T, 256, 2>(v, labels, out, total, stream);
+  return launch_row<T, 256, 8>(v, labels, out, total, stream);
+}
+
+}  // namespace
+
 extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                             int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
                             float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len) {
@@ -97,13 +129,13 @@ extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int6
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
   const ScoreOut out{d_logp, d_lse, d_entropy, d_top_logp, d_top_idx, top_k};
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const int64_t total = (int64_t)K * rows;
+  cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes};
-    logprob_kernel<T><<<(unsigned)total, 256, 0, stream>>>(v, d_labels, out);
+    e = launch_scores<T>(v, d_labels, out, K, stream);
   });
-  return err.launched();
+  return err.done(e);
 }
 
 extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
@@ -135,7 +167,7 @@ extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K,
     const GradOut<T> o{static_cast<T*>(d_dlogits), out_stride_k, out_stride_row, out_stride_class};
     logprob_grad_kernel<T><<<(unsigned)total, 256, 0, stream>>>(v, in, o);
   });
-  return err.launched();
+  return err.done(cudaPeekAtLastError());
 }
 
 namespace {
@@ -215,11 +247,7 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
     cfg.gridDim = dim3((unsigned)ceil_div(total, 32)); cfg.blockDim = dim3(32, 32); cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = 1;
     e = cudaLaunchKernelEx(&cfg, head_join_kernel, a, total, out);
   }
-  if (e != cudaSuccess) {
-    (void)cudaGetLastError();
-    return err.fail(LSAM_ERR_CUDA, cudaGetErrorString(e));
-  }
-  return LSAM_OK;
+  return err.done(e);
 }
 
 extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, int32_t dtype, int32_t K, int64_t rows, int64_t n, int64_t x_stride_k,
@@ -257,5 +285,5 @@ extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, in
     using T = decltype(t);
     dropout_kernel<T><<<(unsigned)ceil_div(total, 256), 256, 0, stream>>>(static_cast<const T*>(d_x), static_cast<const T*>(d_skip), static_cast<T*>(d_out), a, groups, total);
   });
-  return err.launched();
+  return err.done(cudaPeekAtLastError());
 }
