@@ -329,7 +329,7 @@ enum { LSAM_FP32 = 0, LSAM_BF16 = 1, LSAM_FP16 = 2 };
  *  d_labels   nullable int32: a negative label leaves the row out (it is not read; logp = lse = entropy = 0, no alternatives); a
  *             label >= classes makes logp NaN.
  *  d_logp (needs d_labels), d_lse, d_entropy: nullable.  top_k = 0 .. LSAM_TOP_MAX; with 0 the two top arrays are not touched.
- * Logits below -1e30 are masks (-inf, or the lowest value of bf16 and fp32): probability 0, log probability -inf, never alternatives.
+ * Logits at or below -1e30 are masks (-inf, or the lowest value of bf16 and fp32): probability 0, log probability -inf, never alternatives.
  * Missing alternatives have index -1 and log probability -inf; a row of nothing but masks has lse = -inf, logp = -inf, entropy 0.  A NaN or a
  * +inf logit (from 2e38 on) makes lse, entropy and every log probability of its row NaN (a masked label keeps -inf); NaN is never an alternative. */
 #define LSAM_TOP_MAX 32

@@ -5,6 +5,7 @@ There is no CPU fallback: loading fails loudly when the shared library cannot be
 """
 import ctypes as C
 import os
+import threading
 from typing import NamedTuple
 
 import numpy as np
@@ -187,58 +188,64 @@ def _invalid(msg):
     return LsamError(LSAM_ERR_INVALID, msg)
 
 
-def _stacked(t, what):
-    """(K, rows, columns) and the strides of a [rows, columns] or [K, rows, columns] tensor."""
-    if t.dim() == 2:
-        return (1, *t.shape), (0, *t.stride())
-    if t.dim() == 3:
-        return tuple(t.shape), t.stride()
-    raise _invalid(f"{what} must have 2 or 3 dimensions")
+_torch = None
+_codes = {}  # torch dtype -> LSAM_FP32 / LSAM_BF16 / LSAM_FP16
+_err = threading.local()  # one message buffer per thread
 
 
-def _dtype_code(t, what):
-    name = str(t.dtype)
-    try:
-        return {"torch.float32": FP32, "torch.bfloat16": BF16, "torch.float16": FP16}[name]
-    except KeyError:
-        raise _invalid(f"{what}: {name} is not one of float32, bfloat16, float16") from None
-
-
-def _check_like(t, what, shape, dtype, device):
-    if t is None:
-        return None
-    if tuple(t.shape) != tuple(shape) or str(t.dtype) != dtype or t.device != device or not t.is_contiguous():
-        raise _invalid(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
-    return t.data_ptr()
-
-
-class _OnStream:
-    """Allocations inside belong to `stream` (None: the current stream of the device), whose handle is `.handle`."""
-
-    def __init__(self, device, stream):
+def _load():
+    """torch, imported with the first operator call."""
+    global _torch
+    if _torch is None:
         import torch
 
-        if device.type != "cuda":
-            raise _invalid("the operators take CUDA tensors: there is no CPU path")
-        cur = torch.cuda.current_stream(device)
-        self.handle = (stream or cur).cuda_stream
-        self.scope = torch.cuda.stream(stream) if stream is not None and stream != cur else None
-
-    def __enter__(self):
-        if self.scope is not None:
-            self.scope.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.scope is not None:
-            self.scope.__exit__(*exc)
+        _codes.update({torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16})
+        _torch = torch
+    return _torch
 
 
 def _call(fn, *args):
-    err = C.create_string_buffer(256)
-    rc = fn(*args, err, 256)
+    try:
+        buf = _err.buf
+    except AttributeError:
+        buf = _err.buf = C.create_string_buffer(256)
+    rc = fn(*args, buf, 256)
     if rc != LSAM_OK:
-        raise LsamError(rc, err.value.decode())
+        raise LsamError(rc, buf.value.decode())
+
+
+def _stacked(t, what):
+    """K, rows, columns and the strides of a [rows, columns] or [K, rows, columns] tensor."""
+    n = t.dim()
+    if n == 3:
+        return (*t.shape, *t.stride())
+    if n == 2:
+        return (1, *t.shape, 0, *t.stride())
+    raise _invalid(f"{what} must have 2 or 3 dimensions")
+
+
+def _code(t, what):
+    code = _codes.get(t.dtype)
+    if code is None:
+        raise _invalid(f"{what}: {t.dtype} is not one of float32, bfloat16, float16")
+    if not t.is_cuda:
+        raise _invalid("the operators take CUDA tensors: there is no CPU path")
+    return code
+
+
+def _ptr(t, what, shape, dtype, dev):
+    """Address of a dense per-row array, None if it is not given."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != dev:
+        raise _invalid(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    return t.data_ptr()
+
+
+def _on(stream, fn):
+    """Runs an operator with `stream` as the current stream, so that what it allocates belongs to that stream."""
+    with _torch.cuda.stream(stream):
+        return fn()
 
 
 def lsam_logprob(logits, labels=None, top_k=0, stream=None):
@@ -246,26 +253,29 @@ def lsam_logprob(logits, labels=None, top_k=0, stream=None):
 
     logits: [rows, classes] or [K, rows, classes], float32 / bfloat16 / float16, any strides (a context's own logits have the sample
     index contiguous: a transposed view).  labels: int32 [rows] / [K, rows]; negative = the row is left out (zeros, index -1), None = no
-    logp.  The rules for -inf, NaN and ties stand in include/lsam.h.  Returns LogProb.
+    logp.  The rules for masks, NaN and ties stand in include/lsam.h.  Returns LogProb.  stream: None = the current one.
     """
-    import torch
-
-    (K, R, V), (sk, sr, sc) = _stacked(logits, "logits")
-    code = _dtype_code(logits, "logits")
-    lead, dev = logits.shape[:-1], logits.device
-    with _OnStream(dev, stream) as on:
-        pl = _check_like(labels, "labels", lead, "torch.int32", dev)
-        f = torch.empty((3, *lead), dtype=torch.float32, device=dev)
-        tv = ti = None
-        if top_k:
-            if not 0 < top_k <= TOP_MAX:
-                raise _invalid(f"top_k outside 0 .. {TOP_MAX}")
-            tv = torch.empty((*lead, top_k), dtype=torch.float32, device=dev)
-            ti = torch.empty((*lead, top_k), dtype=torch.int32, device=dev)
-        logp, lse, ent = f.unbind(0)
-        _call(lib().lsam_logprob, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, top_k, logp.data_ptr() if pl is not None else None, lse.data_ptr(),
-              ent.data_ptr(), tv.data_ptr() if top_k else None, ti.data_ptr() if top_k else None, on.handle)
-    return LogProb(logp if labels is not None else None, lse, ent, tv, ti)
+    torch = _load()
+    if stream is not None:
+        return _on(stream, lambda: lsam_logprob(logits, labels, top_k))
+    K, R, V, sk, sr, sc = _stacked(logits, "logits")
+    code = _code(logits, "logits")
+    dev = logits.device
+    lead = logits.shape[:-1]
+    pl = None if labels is None else _ptr(labels, "labels", lead, torch.int32, dev)
+    logp = None if labels is None else torch.empty(lead, dtype=torch.float32, device=dev)
+    lse = torch.empty(lead, dtype=torch.float32, device=dev)
+    ent = torch.empty(lead, dtype=torch.float32, device=dev)
+    tv = ti = pv = pi = None
+    if top_k:
+        if not 0 < top_k <= TOP_MAX:
+            raise _invalid(f"top_k outside 0 .. {TOP_MAX}")
+        tv = torch.empty((*lead, top_k), dtype=torch.float32, device=dev)
+        ti = torch.empty((*lead, top_k), dtype=torch.int32, device=dev)
+        pv, pi = tv.data_ptr(), ti.data_ptr()
+    _call(lib().lsam_logprob, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, top_k, None if logp is None else logp.data_ptr(), lse.data_ptr(), ent.data_ptr(), pv, pi,
+          torch.cuda.current_stream(dev).cuda_stream)
+    return LogProb(logp, lse, ent, tv, ti)
 
 
 def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, out=None, stream=None):
@@ -274,22 +284,25 @@ def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, o
     lse and entropy: what lsam_logprob returned for these logits.  out: tensor of the logits' shape and type to write (logits itself is
     allowed), None = a new one.  Returns it.
     """
-    import torch
-
-    (K, R, V), (sk, sr, sc) = _stacked(logits, "logits")
-    code = _dtype_code(logits, "logits")
-    lead, dev = logits.shape[:-1], logits.device
-    with _OnStream(dev, stream) as on:
-        pl = _check_like(labels, "labels", lead, "torch.int32", dev)
-        rows = [_check_like(t, w, lead, "torch.float32", dev) for t, w in ((lse, "lse"), (entropy, "entropy"), (dlogp, "dlogp"), (dentropy, "dentropy"))]
-        if rows[0] is None:
-            raise _invalid("lse is needed")
-        if out is None:
-            out = torch.empty_like(logits)
-        elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
-            raise _invalid("out must have the shape, type and device of logits")
-        _, (ok, orow, oc) = _stacked(out, "out")
-        _call(lib().lsam_logprob_grad, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, *rows, out.data_ptr(), ok, orow, oc, on.handle)
+    torch = _load()
+    if stream is not None:
+        return _on(stream, lambda: lsam_logprob_grad(logits, labels, lse, dlogp, entropy, dentropy, out))
+    K, R, V, sk, sr, sc = _stacked(logits, "logits")
+    code = _code(logits, "logits")
+    dev = logits.device
+    lead = logits.shape[:-1]
+    f32 = torch.float32
+    pl = _ptr(labels, "labels", lead, torch.int32, dev)
+    ps = _ptr(lse, "lse", lead, f32, dev)
+    if ps is None:
+        raise _invalid("lse is needed")
+    pe, pa, pb = _ptr(entropy, "entropy", lead, f32, dev), _ptr(dlogp, "dlogp", lead, f32, dev), _ptr(dentropy, "dentropy", lead, f32, dev)
+    if out is None:
+        out = torch.empty_like(logits)
+    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
+        raise _invalid("out must have the shape, type and device of logits")
+    ok, orow, oc = _stacked(out, "out")[3:]
+    _call(lib().lsam_logprob_grad, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, ps, pe, pa, pb, out.data_ptr(), ok, orow, oc, torch.cuda.current_stream(dev).cuda_stream)
     return out
 
 
@@ -299,29 +312,32 @@ def lsam_head_logprob(h, w, labels=None, bias=None, stream=None):
     h: [rows, inner] or [K, rows, inner]; w: [classes, inner] (shared by the workers) or [K, classes, inner]; bias: fp32 [classes] /
     [K, classes]; the inner index contiguous.  Returns LogProb without alternatives.
     """
-    import torch
-
-    (K, R, D), (hk, hr, hc) = _stacked(h, "h")
-    (KW, V, DW), (wk, wc, wi) = _stacked(w, "w")
-    code = _dtype_code(h, "h")
-    lead, dev = h.shape[:-1], h.device
+    torch = _load()
+    if stream is not None:
+        return _on(stream, lambda: lsam_head_logprob(h, w, labels, bias))
+    K, R, D, hk, hr, hc = _stacked(h, "h")
+    KW, V, DW, wk, wc, wi = _stacked(w, "w")
+    code = _code(h, "h")
+    dev = h.device
+    lead = h.shape[:-1]
     if DW != D or w.dtype != h.dtype or w.device != dev or (w.dim() == 3 and KW != K):
         raise _invalid("w must be [classes, inner] or [K, classes, inner] of the type and device of h")
     if (hc != 1 or wi != 1) and D > 1:
         raise _invalid("the inner index of h and w must be contiguous")
-    with _OnStream(dev, stream) as on:
-        pl = _check_like(labels, "labels", lead, "torch.int32", dev)
-        pb, bk = None, 0
-        if bias is not None:
-            pb = _check_like(bias, "bias", (V,) if bias.dim() == 1 else (K, V), "torch.float32", dev)
-            bk = V if bias.dim() == 2 else 0
-        f = torch.empty((3, *lead), dtype=torch.float32, device=dev)
-        logp, lse, ent = f.unbind(0)
-        nbytes = lib().lsam_head_logprob_workspace_bytes(K, R, V)
-        ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
-        _call(lib().lsam_head_logprob, h.data_ptr(), w.data_ptr(), pb, code, K, R, D, V, hk, hr, wk, wc, bk, pl, logp.data_ptr() if pl is not None else None,
-              lse.data_ptr(), ent.data_ptr(), (ws.data_ptr() + 255) // 256 * 256, nbytes, on.handle)
-    return LogProb(logp if labels is not None else None, lse, ent, None, None)
+    pl = _ptr(labels, "labels", lead, torch.int32, dev)
+    pb, bk = None, 0
+    if bias is not None:
+        pb = _ptr(bias, "bias", (V,) if bias.dim() == 1 else (K, V), torch.float32, dev)
+        bk = V if bias.dim() == 2 else 0
+    logp = None if labels is None else torch.empty(lead, dtype=torch.float32, device=dev)
+    lse = torch.empty(lead, dtype=torch.float32, device=dev)
+    ent = torch.empty(lead, dtype=torch.float32, device=dev)
+    L = lib()
+    nbytes = L.lsam_head_logprob_workspace_bytes(K, R, V)
+    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
+    _call(L.lsam_head_logprob, h.data_ptr(), w.data_ptr(), pb, code, K, R, D, V, hk, hr, wk, wc, bk, pl, None if logp is None else logp.data_ptr(), lse.data_ptr(),
+          ent.data_ptr(), (ws.data_ptr() + 255) // 256 * 256, nbytes, torch.cuda.current_stream(dev).cuda_stream)
+    return LogProb(logp, lse, ent, None, None)
 
 
 def lsam_dropout(x, p, seed, tick, layer=0, k_offset=0, skip=None, out=None, stream=None):
@@ -330,25 +346,29 @@ def lsam_dropout(x, p, seed, tick, layer=0, k_offset=0, skip=None, out=None, str
     x: [rows, n] or [K, rows, n], float32 / bfloat16 / float16, columns contiguous; worker k_offset + k owns x[k].  The backward pass is the
     same call on the gradient, without skip.  out: tensor to write (x or skip itself is allowed), None = a new one.  Returns it.
     """
-    import torch
-
-    (K, R, n), (xk, xr, xc) = _stacked(x, "x")
-    code = _dtype_code(x, "x")
+    torch = _load()
+    if stream is not None:
+        return _on(stream, lambda: lsam_dropout(x, p, seed, tick, layer, k_offset, skip, out))
+    K, R, n, xk, xr, xc = _stacked(x, "x")
+    code = _code(x, "x")
     dev = x.device
-    if not 0 <= int(seed) < 1 << 64 or not 0 <= int(tick) < 1 << 64:
+    if not 0 <= seed < 1 << 64 or not 0 <= tick < 1 << 64:
         raise _invalid("seed and tick are unsigned 64-bit numbers")
-    with _OnStream(dev, stream) as on:
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        for t, what in ((skip, "skip"), (out, "out")):
-            if t is not None and (t.shape != x.shape or t.dtype != x.dtype or t.device != dev):
-                raise _invalid(f"{what} must have the shape, type and device of x")
-        _, (ok, orow, oc) = _stacked(out, "out")
-        (_, (sk, sr, sc)) = _stacked(skip, "skip") if skip is not None else (None, (0, 0, 1))
-        if (xc != 1 or oc != 1 or sc != 1) and n > 1:
-            raise _invalid("the columns of x, skip and out must be contiguous")
-        _call(lib().lsam_dropout, x.data_ptr(), skip.data_ptr() if skip is not None else None, out.data_ptr(), code, K, R, n, xk, xr, sk, sr, ok, orow,
-              p, int(seed), int(tick), int(layer), int(k_offset), on.handle)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    elif out.shape != x.shape or out.dtype != x.dtype or out.device != dev:
+        raise _invalid("out must have the shape, type and device of x")
+    ok, orow, oc = _stacked(out, "out")[3:]
+    ps, sk, sr, sc = None, 0, 0, 1
+    if skip is not None:
+        if skip.shape != x.shape or skip.dtype != x.dtype or skip.device != dev:
+            raise _invalid("skip must have the shape, type and device of x")
+        ps = skip.data_ptr()
+        sk, sr, sc = _stacked(skip, "skip")[3:]
+    if (xc != 1 or oc != 1 or sc != 1) and n > 1:
+        raise _invalid("the columns of x, skip and out must be contiguous")
+    _call(lib().lsam_dropout, x.data_ptr(), ps, out.data_ptr(), code, K, R, n, xk, xr, sk, sr, ok, orow, p, seed, tick, layer, k_offset,
+          torch.cuda.current_stream(dev).cuda_stream)
     return out
 
 

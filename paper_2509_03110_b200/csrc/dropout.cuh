@@ -1,39 +1,135 @@
 // dropout.cuh -- dropout whose mask is a function of (seed, tick, layer, worker, row, column) and is never stored.
+//
+// One Philox4x32-10 block gives the 16-bit numbers of eight columns: the generator's twenty wide multiplications cost about five instructions
+// per element, little enough that the bytes of x, skip and out bound the pass (with 32-bit numbers, four columns a block, it would be ten).
 #pragma once
 
 #include "common.cuh"
+#include "head_ops.cuh"
 
 namespace lsam {
+
+// n / d for n < 2^31 by one multiplication: m = floor(2^s / d) + 1, s = 31 + ceil(log2 d); m d exceeds 2^s by at most d <= 2^(s - 31)
+struct FastDiv {
+  uint64_t m = 1;
+  uint32_t s = 0, d = 1;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t div) : d(div) {
+    uint32_t l = 0;
+    while (((uint64_t)1 << l) < div) ++l;
+    s = 31 + l;
+    m = ((uint64_t)1 << s) / div + 1;
+  }
+  __device__ inline uint32_t div(uint32_t n, uint32_t& rem) const {
+    const uint32_t q = (uint32_t)(n * m >> s);
+    rem = n - q * d;
+    return q;
+  }
+};
 
 struct DropArgs {
   int64_t rows, n;
   int64_t xk, xr, sk, sr, ok, orr;  // strides of x, skip and out: worker, row (columns are contiguous)
   uint32_t key0, key1, tick, word2; // Philox key; counter words 3 and 2 (the latter for worker 0)
-  uint32_t cut;                     // an element is dropped when its 16 bits are below `cut`
+  uint32_t limit;                   // an element is dropped when its 16 bits, moved to the top of a word, are below `limit`
+  bool some;                        // false: everything is dropped
   float scale;                      // 65536 / (65536 - cut)
+  FastDiv by_groups, by_rows;
+  __device__ inline void bits(uint32_t k, uint32_t r, uint32_t g, uint32_t (&w)[4]) const {  // columns 8 g .. 8 g + 7
+    philox4x32_10(g, r, word2 + k, tick, key0, key1, w);
+  }
+  // `top`: the element's 16 bits at the top of a word; what lies below them does not reach the comparison
+  __device__ inline float value(float x, uint32_t top) const { return some && top >= limit ? x * scale : 0.f; }
 };
 
-// The 16 random bits of the eight columns 8 g .. 8 g + 7 of a row: word j / 2 of the Philox block, low half first.
-__device__ inline void drop_bits(const DropArgs& a, int64_t k, int64_t r, int64_t g, uint32_t (&w)[4]) {
-  philox4x32_10((uint32_t)g, (uint32_t)r, a.word2 + (uint32_t)k, a.tick, a.key0, a.key1, w);
-}
+constexpr int kDropUnroll = 2;
 
-// out = skip + (kept ? x * scale : 0); one thread per group of eight columns
+// Every row starts on a 16-byte boundary: a thread owns kDropUnroll groups of eight columns (one 16-byte vector of each tensor, two in fp32); a row's
+// last columns, when they are no whole group, move one by one.
 template <typename T>
 __global__ void __launch_bounds__(256)
-dropout_kernel(const T* x, const T* skip, T* out, DropArgs a, int64_t groups, int64_t total) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= total) return;
-  const int64_t g = e % groups, kr = e / groups, r = kr % a.rows, k = kr / a.rows;
+dropout_vec_kernel(const T* x, const T* skip, T* out, DropArgs a, uint32_t total) {
+  constexpr int NV = (int)sizeof(T) / 2, N = vec_n<T>();  // vectors per group
+#pragma unroll
+  for (int u = 0; u < kDropUnroll; ++u) {
+    const uint32_t e = (blockIdx.x * kDropUnroll + u) * 256u + threadIdx.x;
+    if (e >= total) return;
+    uint32_t g, r;
+    const uint32_t k = a.by_rows.div(a.by_groups.div(e, g), r);
+    const int64_t c = (int64_t)g * 8;
+    const T* xp = x + k * a.xk + r * a.xr + c;
+    const T* sp = skip ? skip + k * a.sk + r * a.sr + c : nullptr;
+    T* op = out + k * a.ok + r * a.orr + c;
+    uint32_t w[4];
+    if (c + 8 <= a.n) {
+      uint4 xv[NV], sv[NV];
+#pragma unroll
+      for (int q = 0; q < NV; ++q) {
+        xv[q] = reinterpret_cast<const uint4*>(xp)[q];
+        if (sp) sv[q] = reinterpret_cast<const uint4*>(sp)[q];
+      }
+      a.bits(k, r, g, w);
+#pragma unroll
+      for (int q = 0; q < NV; ++q) {
+        float v[N];
+        vec_unpack<T>(xv[q], v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const int b = q * N + j;
+          v[j] = a.value(v[j], (b & 1) ? w[b >> 1] : w[b >> 1] << 16);
+        }
+        if (sp) {
+          float s[N];
+          vec_unpack<T>(sv[q], s);
+#pragma unroll
+          for (int j = 0; j < N; ++j) v[j] += s[j];
+        }
+        reinterpret_cast<uint4*>(op)[q] = vec_pack<T>(v);
+      }
+    } else {
+      a.bits(k, r, g, w);
+#pragma unroll
+      for (int b = 0; b < 8; ++b)
+        if (c + b < a.n) {
+          float v = a.value(to_float(xp[b]), (b & 1) ? w[b >> 1] : w[b >> 1] << 16);
+          if (sp) v += to_float(sp[b]);
+          op[b] = from_float<T>(v);
+        }
+    }
+  }
+}
+
+// Any alignment: a warp takes 256 columns of a row.  Lane i draws the numbers of its group of eight and leaves them in shared memory, so that
+// consecutive lanes move consecutive elements.
+template <typename T>
+__global__ void __launch_bounds__(256)
+dropout_elem_kernel(const T* x, const T* skip, T* out, DropArgs a, int64_t segments, int64_t total) {
+  __shared__ __align__(16) uint16_t num[8][256];
+  const int wp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t unit = (int64_t)blockIdx.x * 8 + wp;
+  if (unit >= total) return;
+  const int64_t seg = unit % segments, kr = unit / segments, r = kr % a.rows, k = kr / a.rows, c0 = seg * 256 + lane;
+  const T* xp = x + k * a.xk + r * a.xr;
+  const T* sp = skip ? skip + k * a.sk + r * a.sr : nullptr;
+  T* op = out + k * a.ok + r * a.orr;
+  float v[8], s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const bool in = c0 + e * 32 < a.n;
+    v[e] = in ? to_float(xp[c0 + e * 32]) : 0.f;
+    s[e] = in && sp ? to_float(sp[c0 + e * 32]) : 0.f;
+  }
   uint32_t w[4];
-  drop_bits(a, k, r, g, w);
-  for (int j = 0; j < 8; ++j) {
-    const int64_t c = g * 8 + j;
+  a.bits((uint32_t)k, (uint32_t)r, (uint32_t)(seg * 32 + lane), w);
+  *reinterpret_cast<uint4*>(&num[wp][lane * 8]) = make_uint4(w[0], w[1], w[2], w[3]);
+  __syncwarp();
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int64_t c = c0 + e * 32;
     if (c >= a.n) break;
-    const uint32_t bits = (w[j >> 1] >> (16 * (j & 1))) & 0xffffu;
-    float y = bits >= a.cut ? to_float(x[k * a.xk + r * a.xr + c]) * a.scale : 0.f;
-    if (skip) y += to_float(skip[k * a.sk + r * a.sr + c]);
-    out[k * a.ok + r * a.orr + c] = from_float<T>(y);
+    float y = a.value(v[e], (uint32_t)num[wp][lane + e * 32] << 16);
+    if (sp) y += s[e];
+    op[c] = from_float<T>(y);
   }
 }
 

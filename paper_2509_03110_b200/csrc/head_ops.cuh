@@ -22,7 +22,7 @@ __device__ inline float ex2(float x) {
 // and w = l k - B (one fused multiply-add):  s = sum 2^w,  t = sum 2^w w,  so that
 //   logsumexp = m + (log2 s - (m k - B)) / k,   entropy = -sum p log p = (log2 s - t / s) / k.
 // B is the reference itself, not an approximation of m k, and k's own rounding only scales the logits by 1 + 1e-8: an offset common to all
-// logits costs no digits of the entropy or of a log probability.  Logits below kMasked are masks: they enter as kMasked, whose 2^w is 0
+// logits costs no digits of the entropy or of a log probability.  Logits at or below kMasked are masks: they enter as kMasked, whose 2^w is 0
 // beside any other (and (-inf) * 0 never arises); a set of nothing but masks has m = kMasked.  A NaN or +inf logit makes s NaN.
 constexpr float kMasked = -1e30f;
 struct RowStat { float m, s, t; };
@@ -62,7 +62,7 @@ __device__ inline RowScore stat_finish(const RowStat& a) {
   const float B = a.m * kLog2e, ls = log2f(a.s);
   return {B, ls, a.m + (ls - fmaf(a.m, kLog2e, -B)) / kLog2e, (ls - a.t / a.s) / kLog2e};
 }
-__device__ inline float score_logp(float l, const RowScore& r) { return l < kMasked ? -INFINITY : (fmaf(l, kLog2e, -r.B) - r.ls) / kLog2e; }
+__device__ inline float score_logp(float l, const RowScore& r) { return l <= kMasked ? -INFINITY : (fmaf(l, kLog2e, -r.B) - r.ls) / kLog2e; }
 
 // Order of the alternatives: larger logit first, then the lower class.  One 64-bit key per element (0: not an alternative,
 // i.e. a mask or NaN); -0 and +0 are one value.
@@ -72,7 +72,7 @@ __device__ inline uint32_t order_bits(float v) {
 }
 __device__ inline float order_value(uint32_t o) { return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
 __device__ inline uint64_t order_key(float v, int32_t c) {
-  return v >= kMasked ? ((uint64_t)order_bits(v) << 32) | (uint32_t)~c : 0ull;
+  return v > kMasked ? ((uint64_t)order_bits(v) << 32) | (uint32_t)~c : 0ull;
 }
 
 // Logits of one call: element (k, r, c) at p[k * sk + r * sr + c * sc]; row index = k * rows + r.
@@ -219,11 +219,13 @@ struct RowParts {
   }
   __device__ inline float at(int64_t c) const { return to_float(row[c * sc]); }
   __device__ inline uint4 vec(int32_t v) const { return __ldg(reinterpret_cast<const uint4*>(row + head) + v); }
-  // f(value, class) for every element that thread g of G owns; the warp's lanes take its vectors in turn
+  // f(value, class) for every element that thread g of G owns; `lanes` threads take its vectors in turn
   template <class F>
-  __device__ inline void each_of(int g, int G, int lane, F&& f) const {
-    for (int64_t c = g + (int64_t)lane * G; c < head; c += 32 * (int64_t)G) f(at(c), (int32_t)c);
-    for (int64_t v = g + (int64_t)lane * G; v < nvec; v += 32 * (int64_t)G) {
+  __device__ inline void each_of(int g, int G, int lane, int lanes, F&& f) const {
+    const int64_t step = (int64_t)lanes * G;
+    for (int64_t c = g + (int64_t)lane * G; c < head; c += step) f(at(c), (int32_t)c);
+#pragma unroll 2
+    for (int64_t v = g + (int64_t)lane * G; v < nvec; v += step) {
       const uint4 q = vec((int32_t)v);
       float l[vec_n<T>()];
       vec_unpack<T>(q, l);
@@ -288,18 +290,27 @@ __device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, int k,
     __syncthreads();
     thr = order_value(sh.thr);
   }
-  if (vm >= thr) sh.owners[atomicAdd(&sh.n_own, 1)] = tid;
+  const bool owner = vm >= thr && vm > kMasked;
+  if (owner) sh.owners[atomicAdd(&sh.n_own, 1)] = tid;
   __syncthreads();
-  for (int q = w; q < sh.n_own; q += NW)
-    rp.each_of(g0 + sh.owners[q], G, lane, [&](float l, int32_t c) {
-      if (l > thr) {
-        const int at = atomicAdd(&sh.n_above, 1);
-        if (at < LIST) sh.above[at] = order_key(l, c);
-      } else if (l == thr) {
-        const int at = atomicAdd(&sh.n_equal, 1);
-        if (at < LIST) sh.equal[at] = order_key(l, c);
-      }
-    });
+  const int n_own = sh.n_own;
+  // few owners: a warp takes one at a time, its lanes read the owner's vectors side by side; many (tied rows): every owner reads its own
+  auto each_candidate = [&](auto&& f) {
+    if (n_own <= 8 * NW) {
+      for (int q = w; q < n_own; q += NW) rp.each_of(g0 + sh.owners[q], G, lane, 32, f);
+    } else if (owner) {
+      rp.each_of(g0 + tid, G, 0, 1, f);
+    }
+  };
+  each_candidate([&](float l, int32_t c) {
+    if (l > thr) {
+      const int at = atomicAdd(&sh.n_above, 1);
+      if (at < LIST) sh.above[at] = order_key(l, c);
+    } else if (l == thr && l > kMasked) {
+      const int at = atomicAdd(&sh.n_equal, 1);
+      if (at < LIST) sh.equal[at] = order_key(l, c);
+    }
+  });
   __syncthreads();
   const int na = sh.n_above, ne = sh.n_equal;
   if (na > LIST) {
@@ -310,7 +321,7 @@ __device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, int k,
         const uint64_t key = order_key(l, c);
         if (key < last && key > best) best = key;
       };
-      for (int q = w; q < sh.n_own; q += NW) rp.each_of(g0 + sh.owners[q], G, lane, see);
+      each_candidate(see);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) best = max(best, (uint64_t)__shfl_xor_sync(~0u, (unsigned long long)best, d));
       __syncthreads();
@@ -390,11 +401,11 @@ __device__ inline void write_top(const ScoreOut& o, int64_t i, int j, uint64_t k
 }
 
 // Rows of contiguous classes: NT threads of CS blocks (a cluster) per row, one pass.  A thread keeps the statistics of the vectors it owns in
-// registers, four (fp32: eight) vectors per step so that 64 (128) bytes a thread are in flight; nothing is exchanged until the row ends.
+// registers, four per step with the next four in flight; nothing is exchanged until the row ends.
 template <typename T, int NT, int CS>
 __global__ void __launch_bounds__(NT)
 logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o) {
-  constexpr int NW = NT / 32, U = 4 * (int)sizeof(T) / 2, G = NT * CS;
+  constexpr int NW = NT / 32, U = 4, G = NT * CS;
   __shared__ RowStat ws[NW], cta;
   __shared__ TopShared<NT> sh;
   const int64_t i = blockIdx.x / CS;
@@ -410,10 +421,18 @@ logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut 
   for (int64_t c = g; c < rp.head; c += G) stat_add(a, rp.at(c));
   if ((int64_t)rp.tail0 + g < rp.classes) stat_add(a, rp.at(rp.tail0 + g));
   int64_t q = g;
-  for (; q + (U - 1) * G < rp.nvec; q += U * G) {
+  if (q + (U - 1) * G < rp.nvec) {
     uint4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) x[u] = rp.vec((int32_t)q + u * G);
+    for (q += U * G; q + (U - 1) * G < rp.nvec; q += U * G) {  // the next step's loads fly while this one's vectors are added
+      uint4 n[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) n[u] = rp.vec((int32_t)q + u * G);
+      stat_add_vecs<T, U>(a, x);
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = n[u];
+    }
     stat_add_vecs<T, U>(a, x);
   }
   for (; q < rp.nvec; q += G) {
@@ -466,7 +485,7 @@ logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut 
 // of 16 consecutive samples.  A chunk of 32 x kFeatN classes is loaded into registers in one go, and stays there for the alternatives when it is the whole row.
 constexpr int kFeatR = 16, kFeatG = 32, kFeatN = 32, kFeatList = 48;
 template <typename T>
-__global__ void __launch_bounds__(kFeatR * kFeatG)
+__global__ void __launch_bounds__(kFeatR * kFeatG, 2)
 logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o, int row_blocks) {
   __shared__ float red[3][kFeatR][kFeatG + 1];
   __shared__ uint64_t list[kFeatR][kFeatList];
@@ -489,13 +508,12 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
       const int64_t c = c0 + y + kFeatG * j;
       l[j] = live && c < v.classes ? to_float(p[c * v.sc]) : -INFINITY;
     }
-    float m[kFeatN];  // l itself keeps the masks' own values for the alternatives
 #pragma unroll
     for (int j = 0; j < kFeatN; ++j) {
-      m[j] = max_nan(l[j], kMasked);
-      mx = fmaxf(mx, m[j]);
+      l[j] = max_nan(l[j], kMasked);
+      mx = fmaxf(mx, l[j]);
     }
-    stat_add_all(a, m, mx);
+    stat_add_all(a, l, mx);
   }
   const float vm = a.m;
   red[0][x][y] = a.m; red[1][x][y] = a.s; red[2][x][y] = a.t;
@@ -523,12 +541,12 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
   __syncthreads();
   const float thr = thr_s[x];
   auto offer = [&](float val, int64_t c) {
-    if (val >= thr && val >= kMasked) {
+    if (val >= thr && val > kMasked) {
       const int at = atomicAdd(&count[x], 1);
       if (at < kFeatList) list[x][at] = order_key(val, (int32_t)c);
     }
   };
-  if (live && vm >= thr) {
+  if (live && vm >= thr && vm > kMasked) {
     if (v.classes <= kFeatG * kFeatN) {
 #pragma unroll
       for (int j = 0; j < kFeatN; ++j) offer(l[j], y + kFeatG * j);
@@ -567,6 +585,8 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
 
 // Gradient of L(logp, entropy) of every row:  dl_c = a (1[c = y] - p_c) - b p_c (log p_c + H),  p_c = e^(l_c - lse),
 // a = dL/dlogp, b = dL/dH (each nullable = 0).  Rows that are left out (y < 0) or hold nothing but masks (lse = -inf) get 0.
+// With u = l - lse it is p (c0 + c1 u), c0 = -(a + b H), c1 = -b, plus a at the label: one read, one write, two multiply-adds and one exponential
+// per element, bound by the bytes.
 struct GradIn {
   const int32_t* labels;
   const float *lse, *entropy, *dlogp, *dentropy;
@@ -574,25 +594,131 @@ struct GradIn {
 template <typename T>
 struct GradOut { T* p; int64_t sk, sr, sc; };
 
-template <typename T>
+struct GradRow {
+  float lse, c0, c1, at_label;
+  int32_t y;   // class that receives at_label, -1: none
+  bool none;   // all zeros
+  __device__ inline GradRow() : lse(0.f), c0(0.f), c1(0.f), at_label(0.f), y(-1), none(true) {}
+  __device__ inline GradRow(const GradIn& g, int64_t i, int32_t classes) {
+    y = g.labels ? g.labels[i] : -1;
+    lse = g.lse[i];
+    none = (g.labels && y < 0) || lse == -INFINITY;
+    const float a = g.dlogp ? g.dlogp[i] : 0.f;
+    const float b = g.dentropy ? g.dentropy[i] : 0.f;
+    c0 = -a - (g.dentropy ? b * g.entropy[i] : 0.f);
+    c1 = -b;
+    at_label = a;
+    if (y >= classes) c0 = NAN;  // the whole row
+  }
+  __device__ inline float operator()(float l, int64_t c) const {
+    const float u = max_nan(l - lse, -200.f);  // e^-200 is 0 in 32 bits, and (-inf) * 0 never arises
+    const float p = ex2(u * kLog2e);
+    float d = p * fmaf(c1, u, c0);
+    if (c == y) d += at_label;
+    return none ? 0.f : d;
+  }
+};
+
+template <typename T> __device__ inline uint4 vec_pack(const float (&f)[16 / sizeof(T)]) {
+  uint4 q;
+  T* t = reinterpret_cast<T*>(&q);
+#pragma unroll
+  for (int j = 0; j < (int)(16 / sizeof(T)); ++j) t[j] = from_float<T>(f[j]);
+  return q;
+}
+
+// Rows of contiguous classes.  NT = 256: a block takes a chunk of a row, 32: a warp does (eight rows per block).  VEC: input and output rows have the
+// same 16-byte phase (the host checks the strides), so that both move as vectors; else consecutive lanes move consecutive elements.
+template <bool VEC, typename T> __host__ __device__ constexpr int64_t grad_chunk(int NT) { return VEC ? (int64_t)NT * 4 * vec_n<T>() : (int64_t)NT * 8; }
+template <typename T, int NT, bool VEC>
 __global__ void __launch_bounds__(256)
-logprob_grad_kernel(LogitView<T> v, GradIn g, GradOut<T> out) {
-  const int64_t i = blockIdx.x;
-  const int32_t y = g.labels ? g.labels[i] : v.classes - 1;
-  const float lse = g.lse[i];
+grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, int64_t chunks, int64_t units) {
+  constexpr int N = vec_n<T>();
+  const int64_t unit = NT == 32 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
+  if (unit >= units) return;
+  const int t = threadIdx.x % NT;
+  const int64_t i = unit / chunks, chunk = unit % chunks;
+  const GradRow row(g, i, v.classes);
+  const T* src = v.row(i);
   T* dst = out.p + (i / v.rows) * out.sk + (i % v.rows) * out.sr;
-  const bool none = y < 0 || lse < kMasked;
-  const T* row = v.row(i);
-  const float a = g.dlogp ? g.dlogp[i] : 0.f, b = g.dentropy ? g.dentropy[i] : 0.f, H = g.dentropy ? g.entropy[i] : 0.f;
-  const float bad = y >= v.classes ? NAN : 0.f;
-  for (int c = threadIdx.x; c < v.classes; c += 256) {
-    float d = 0.f;
-    if (!none) {
-      const float u = max_nan(to_float(row[c * v.sc]), kMasked) - lse;
-      const float p = ex2(u * kLog2e);
-      d = a * ((c == y ? 1.f : 0.f) - p) - b * (p * (u + H)) + bad;
+  if (VEC) {
+    const RowParts<T> rp(src, 1, v.classes);
+    const int64_t q0 = chunk * NT * 4 + t;
+    uint4 x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (q0 + e * NT < rp.nvec) x[e] = reinterpret_cast<const uint4*>(src + rp.head)[q0 + e * NT];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t q = q0 + e * NT;
+      if (q >= rp.nvec) break;
+      float l[N];
+      vec_unpack<T>(x[e], l);
+      const int64_t c = rp.head + q * N;
+#pragma unroll
+      for (int j = 0; j < N; ++j) l[j] = row(l[j], c + j);
+      reinterpret_cast<uint4*>(dst + rp.head)[q] = vec_pack<T>(l);
     }
-    dst[c * out.sc] = from_float<T>(d);
+    if (chunk == 0) {  // both are shorter than a vector
+      if (t < rp.head) dst[t] = from_float<T>(row(to_float(src[t]), t));
+      const int64_t c = (int64_t)rp.tail0 + t;
+      if (c < v.classes) dst[c] = from_float<T>(row(to_float(src[c]), c));
+    }
+  } else {
+    float l[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t c = (chunk * 8 + e) * NT + t;
+      l[e] = c < v.classes ? to_float(src[c * v.sc]) : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t c = (chunk * 8 + e) * NT + t;
+      if (c < v.classes) dst[c * out.sc] = from_float<T>(row(l[e], c));
+    }
+  }
+}
+
+// Logits and gradient with the sample index contiguous: a thread owns R consecutive rows (a 16-byte vector, or one row where the strides do
+// not allow it) and 8 classes of a block's 64.  block (32, 8), grid K * row blocks * class blocks.
+template <typename T, int R>
+__global__ void __launch_bounds__(256)
+grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_blocks, uint32_t class_blocks) {
+  const uint32_t cb = blockIdx.x % class_blocks, kr = blockIdx.x / class_blocks, rb = kr % row_blocks, k = kr / row_blocks;
+  const int64_t r0 = ((int64_t)rb * 32 + threadIdx.x) * R;
+  if (r0 >= v.rows) return;
+  const T* src = v.p + k * v.sk + r0;
+  T* dst = out.p + k * out.sk + r0;
+  GradRow row[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j)
+    if (r0 + j < v.rows) row[j] = GradRow(g, (int64_t)k * v.rows + r0 + j, v.classes);
+  const int64_t c0 = (int64_t)cb * 64 + threadIdx.y;
+  if (R > 1 && r0 + R <= v.rows) {
+    constexpr int N = vec_n<T>();
+    static_assert(R == 1 || R == N, "one vector of rows");
+    uint4 x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c0 + 8 * e < v.classes) x[e] = *reinterpret_cast<const uint4*>(src + (c0 + 8 * e) * v.sc);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t c = c0 + 8 * e;
+      if (c >= v.classes) break;
+      float l[N];
+      vec_unpack<T>(x[e], l);
+#pragma unroll
+      for (int j = 0; j < N; ++j) l[j] = row[R > 1 ? j : 0](l[j], c);
+      *reinterpret_cast<uint4*>(dst + c * out.sc) = vec_pack<T>(l);
+    }
+  } else {
+    for (int e = 0; e < 8; ++e) {
+      const int64_t c = c0 + 8 * e;
+      if (c >= v.classes) break;
+#pragma unroll
+      for (int j = 0; j < R; ++j)
+        if (r0 + j < v.rows) dst[c * out.sc + j] = from_float<T>(row[j](to_float(src[c * v.sc + j]), c));
+    }
   }
 }
 

@@ -138,6 +138,39 @@ extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int6
   return err.done(e);
 }
 
+namespace {
+
+// Form of a gradient call: vectors along the classes or along the samples where both tensors have that index contiguous and every row of
+// the two starts at the same place of a 16-byte vector, single elements in the same order otherwise.
+template <typename T>
+cudaError_t launch_grad(const LogitView<T>& v, const GradIn& in, const GradOut<T>& o, int32_t K, cudaStream_t stream) {
+  const int64_t total = (int64_t)K * v.rows;
+  const auto aligned = [](int64_t elems) { return elems * (int64_t)sizeof(T) % 16 == 0; };
+  const uintptr_t pi = reinterpret_cast<uintptr_t>(v.p), po = reinterpret_cast<uintptr_t>(o.p);
+  if (v.sc != 1 && v.sr == 1 && o.sr == 1 && v.rows > 1) {
+    const bool vec = pi % 16 == 0 && po % 16 == 0 && aligned(v.sc) && aligned(o.sc) && (K == 1 || (aligned(v.sk) && aligned(o.sk)));
+    const int64_t class_blocks = ceil_div(v.classes, 64), row_blocks = ceil_div(v.rows, vec ? 32 * vec_n<T>() : 32);
+    if (class_blocks * row_blocks <= kMaxIndex / K) {
+      const unsigned grid = (unsigned)(class_blocks * row_blocks * K);
+      if (vec) grad_feature_kernel<T, vec_n<T>()><<<grid, dim3(32, 8), 0, stream>>>(v, in, o, (uint32_t)row_blocks, (uint32_t)class_blocks);
+      else grad_feature_kernel<T, 1><<<grid, dim3(32, 8), 0, stream>>>(v, in, o, (uint32_t)row_blocks, (uint32_t)class_blocks);
+      return cudaPeekAtLastError();
+    }
+  }
+  const bool vec = v.sc == 1 && o.sc == 1 && (pi - po) % 16 == 0 && (v.rows == 1 || aligned(v.sr - o.sr)) && (K == 1 || aligned(v.sk - o.sk));
+  const bool narrow = v.classes <= 1024;  // a warp per row
+  const auto go = [&](auto kern, int64_t chunk) {
+    const int64_t chunks = ceil_div(v.classes, chunk), units = total * chunks, blocks = narrow ? ceil_div(units, 8) : units;
+    if (blocks > kMaxIndex) return cudaErrorInvalidConfiguration;
+    kern<<<(unsigned)blocks, 256, 0, stream>>>(v, in, o, chunks, units);
+    return cudaPeekAtLastError();
+  };
+  if (vec) return narrow ? go(grad_row_kernel<T, 32, true>, grad_chunk<true, T>(32)) : go(grad_row_kernel<T, 256, true>, grad_chunk<true, T>(256));
+  return narrow ? go(grad_row_kernel<T, 32, false>, grad_chunk<false, T>(32)) : go(grad_row_kernel<T, 256, false>, grad_chunk<false, T>(256));
+}
+
+}  // namespace
+
 extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                                  int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
                                  const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
@@ -160,14 +193,14 @@ extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K,
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
   const GradIn in{d_labels, d_lse, d_entropy, d_dlogp, d_dentropy};
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const int64_t total = (int64_t)K * rows;
+  cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes};
     const GradOut<T> o{static_cast<T*>(d_dlogits), out_stride_k, out_stride_row, out_stride_class};
-    logprob_grad_kernel<T><<<(unsigned)total, 256, 0, stream>>>(v, in, o);
+    e = launch_grad<T>(v, in, o, K, stream);
   });
-  return err.done(cudaPeekAtLastError());
+  return err.done(e);
 }
 
 namespace {
@@ -250,6 +283,32 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
   return err.done(e);
 }
 
+namespace {
+
+// Vectors where every row of the three tensors starts on a 16-byte boundary, else single elements.
+template <typename T>
+cudaError_t launch_dropout(const T* x, const T* skip, T* out, DropArgs a, int32_t K, cudaStream_t stream) {
+  const auto aligned = [&](const T* p, int64_t sk, int64_t sr) {
+    const int64_t es = sizeof(T);
+    return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && (K == 1 || sk * es % 16 == 0) && (a.rows == 1 || sr * es % 16 == 0));
+  };
+  if (aligned(x, a.xk, a.xr) && aligned(skip, a.sk, a.sr) && aligned(out, a.ok, a.orr)) {
+    const int64_t groups = ceil_div(a.n, 8), total = groups * a.rows * K;
+    if (total < kMaxIndex) {
+      a.by_groups = FastDiv((uint32_t)groups);
+      a.by_rows = FastDiv((uint32_t)a.rows);
+      dropout_vec_kernel<T><<<(unsigned)ceil_div(total, 256 * kDropUnroll), 256, 0, stream>>>(x, skip, out, a, (uint32_t)total);
+      return cudaPeekAtLastError();
+    }
+  }
+  const int64_t segments = ceil_div(a.n, 256), total = segments * a.rows * K;
+  if (ceil_div(total, 8) > kMaxIndex) return cudaErrorInvalidConfiguration;
+  dropout_elem_kernel<T><<<(unsigned)ceil_div(total, 8), 256, 0, stream>>>(x, skip, out, a, segments, total);
+  return cudaPeekAtLastError();
+}
+
+}  // namespace
+
 extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, int32_t dtype, int32_t K, int64_t rows, int64_t n, int64_t x_stride_k,
                             int64_t x_stride_row, int64_t skip_stride_k, int64_t skip_stride_row, int64_t out_stride_k, int64_t out_stride_row, double p,
                             uint64_t seed, uint64_t tick, int32_t layer, int32_t k_offset, void* cuda_stream, char* h_err, size_t h_err_len) {
@@ -265,8 +324,7 @@ extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, in
       (d_skip && !strides_ok(K, skip_stride_k, rows, skip_stride_row, n, 1)))
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
   if ((K > 1 && out_stride_k == 0) || (rows > 1 && out_stride_row < n)) return err.fail(LSAM_ERR_INVALID, "elements of the output share an address");
-  const int64_t groups = ceil_div(n, 8);
-  if ((__int128)groups * rows * K >= ((__int128)1 << 38)) return err.fail(LSAM_ERR_INVALID, "K * rows * ceil(n / 8) must be below 2^38");
+  if ((__int128)ceil_div(n, 8) * rows * K >= ((__int128)1 << 38)) return err.fail(LSAM_ERR_INVALID, "K * rows * ceil(n / 8) must be below 2^38");
   PtrCheck pc;
   pc.need(d_x, dtype_size(dtype)); pc.need(d_out, dtype_size(dtype)); pc.optional(d_skip, dtype_size(dtype));
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
@@ -277,13 +335,15 @@ extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, in
   a.key1 = (uint32_t)(seed >> 32) ^ (uint32_t)(tick >> 32);
   a.tick = (uint32_t)tick;
   a.word2 = ((uint32_t)layer << 20) + (uint32_t)k_offset;
-  a.cut = (uint32_t)std::floor(p * 65536.0 + 0.5);
-  a.scale = a.cut < 65536u ? 65536.f / (float)(65536u - a.cut) : 0.f;
+  const uint32_t cut = (uint32_t)std::floor(p * 65536.0 + 0.5);
+  a.some = cut < 65536u;
+  a.limit = a.some ? cut << 16 : 0u;
+  a.scale = a.some ? 65536.f / (float)(65536u - cut) : 0.f;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const int64_t total = groups * rows * K;
+  cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    dropout_kernel<T><<<(unsigned)ceil_div(total, 256), 256, 0, stream>>>(static_cast<const T*>(d_x), static_cast<const T*>(d_skip), static_cast<T*>(d_out), a, groups, total);
+    e = launch_dropout<T>(static_cast<const T*>(d_x), static_cast<const T*>(d_skip), static_cast<T*>(d_out), a, K, stream);
   });
-  return err.done(cudaPeekAtLastError());
+  return err.done(e);
 }

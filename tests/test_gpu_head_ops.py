@@ -34,7 +34,7 @@ def reference(l, labels, top_k):
     """Scores in 64 bits of the stored values, and the bounds of their errors."""
     C = l.shape[-1]
     d = l.double()
-    d = torch.where(d < -1e30, torch.full_like(d, NINF), d)  # masks
+    d = torch.where(d <= -1e30, torch.full_like(d, NINF), d)  # masks
     m = torch.where(torch.isnan(d), torch.full_like(d, NINF), d).amax(-1, keepdim=True)
     base = torch.where(torch.isneginf(m), torch.zeros_like(m), m)
     z = (d - base).exp().sum(-1, keepdim=True).log()  # a +inf logit makes it NaN
@@ -275,7 +275,7 @@ def head_reference(h, w, bias, y):
     mag = h.double().abs() @ w.double().abs().transpose(-1, -2)
     if bias is not None:
         l = l + (bias.double().unsqueeze(-2) if bias.dim() == 2 else bias.double())
-    l = torch.where(l < -1e30, torch.full_like(l, NINF), l)
+    l = torch.where(l <= -1e30, torch.full_like(l, NINF), l)
     # fp32 accumulation, in the tensor cores with truncated addends: at most one step of the running magnitude per term
     l_err = (2 * U * (h.shape[-1] + 8) * mag).amax(-1)
     out = reference(l, y, 0)
