@@ -27,6 +27,25 @@ __device__ inline void grid_dep_sync() { grid_dep_launch(); grid_dep_wait(); }
 __host__ __device__ inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// ---- division by a number the host knows
+// n / d for n < 2^31 by one multiplication: m = floor(2^s / d) + 1, s = 31 + ceil(log2 d); m d exceeds 2^s by at most d <= 2^(s - 31)
+struct FastDiv {
+  uint64_t m = 1;
+  uint32_t s = 0, d = 1;
+  FastDiv() = default;
+  __host__ explicit FastDiv(uint32_t div) : d(div) {
+    uint32_t l = 0;
+    while (((uint64_t)1 << l) < div) ++l;
+    s = 31 + l;
+    m = ((uint64_t)1 << s) / div + 1;
+  }
+  __device__ inline uint32_t div(uint32_t n, uint32_t& rem) const {
+    const uint32_t q = (uint32_t)(n * m >> s);
+    rem = n - q * d;
+    return q;
+  }
+};
+
 // ---- schedule hash (integer, bit-exact): SplitMix64 finaliser chained over (seed ^ tag, t, k * 2^20 + j)
 __host__ __device__ inline uint64_t mix64(uint64_t z) {
   z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ULL;

@@ -9,24 +9,6 @@
 
 namespace lsam {
 
-// n / d for n < 2^31 by one multiplication: m = floor(2^s / d) + 1, s = 31 + ceil(log2 d); m d exceeds 2^s by at most d <= 2^(s - 31)
-struct FastDiv {
-  uint64_t m = 1;
-  uint32_t s = 0, d = 1;
-  FastDiv() = default;
-  explicit FastDiv(uint32_t div) : d(div) {
-    uint32_t l = 0;
-    while (((uint64_t)1 << l) < div) ++l;
-    s = 31 + l;
-    m = ((uint64_t)1 << s) / div + 1;
-  }
-  __device__ inline uint32_t div(uint32_t n, uint32_t& rem) const {
-    const uint32_t q = (uint32_t)(n * m >> s);
-    rem = n - q * d;
-    return q;
-  }
-};
-
 struct DropArgs {
   int64_t rows, n;
   int64_t xk, xr, sk, sr, ok, orr;  // strides of x, skip and out: worker, row (columns are contiguous)

@@ -56,6 +56,21 @@ __device__ inline RowStat stat_merge(RowStat a, RowStat b) {
 __device__ inline RowStat stat_shfl_xor(const RowStat& a, int d) {
   return {__shfl_xor_sync(~0u, a.m, d), __shfl_xor_sync(~0u, a.s, d), __shfl_xor_sync(~0u, a.t, d)};
 }
+__device__ inline float warp_max_f(float v) {  // NaN ignored
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(v));
+  return y;
+}
+// The statistics of a warp's 32 sets, in every lane: one rebase to the common maximum, then two sums in the order of the xor tree.
+__device__ inline RowStat warp_stat(RowStat a) {
+  stat_rebase(a, warp_max_f(a.m));
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    a.s += __shfl_xor_sync(~0u, a.s, d);
+    a.t += __shfl_xor_sync(~0u, a.t, d);
+  }
+  return a;
+}
 struct RowScore { float B, ls, lse, ent; };
 __device__ inline RowScore stat_finish(const RowStat& a) {
   if (a.m <= kMasked && a.s == a.s) return {0.f, 0.f, -INFINITY, 0.f};
@@ -75,13 +90,18 @@ __device__ inline uint64_t order_key(float v, int32_t c) {
   return v > kMasked ? ((uint64_t)order_bits(v) << 32) | (uint32_t)~c : 0ull;
 }
 
-// Logits of one call: element (k, r, c) at p[k * sk + r * sr + c * sc]; row index = k * rows + r.
+// Logits of one call: element (k, r, c) at p[k * sk + r * sr + c * sc]; row index i = k * rows + r < 2^31.
 template <typename T>
 struct LogitView {
   const T* p;
   int64_t rows, sk, sr, sc;
   int32_t classes;
-  __device__ inline const T* row(int64_t i) const { return p + (i / rows) * sk + (i % rows) * sr; }
+  FastDiv by_rows;
+  __device__ inline const T* row(uint32_t i) const {
+    uint32_t r;
+    const uint32_t k = by_rows.div(i, r);
+    return p + k * sk + r * sr;
+  }
 };
 struct ScoreOut {
   float *logp, *lse, *entropy, *top_logp;  // each nullable
@@ -219,94 +239,105 @@ struct RowParts {
   }
   __device__ inline float at(int64_t c) const { return to_float(row[c * sc]); }
   __device__ inline uint4 vec(int32_t v) const { return __ldg(reinterpret_cast<const uint4*>(row + head) + v); }
-  // f(value, class) for every element that thread g of G owns; `lanes` threads take its vectors in turn
+  // f(value, class) for every element >= thr that thread g of G owns; `lanes` threads take its vectors in turn
   template <class F>
-  __device__ inline void each_of(int g, int G, int lane, int lanes, F&& f) const {
-    const int64_t step = (int64_t)lanes * G;
-    for (int64_t c = g + (int64_t)lane * G; c < head; c += step) f(at(c), (int32_t)c);
+  __device__ inline void each_of(int g, int G, int lane, int lanes, float thr, F&& f) const {
+    auto see = [&](float l, int32_t c) {
+      if (l >= thr) f(l, c);
+    };
+    if (head > 0)
+      for (int64_t c = g + (int64_t)lane * G; c < head; c += (int64_t)lanes * G) see(at(c), (int32_t)c);
+    const int32_t step = lanes * G;
 #pragma unroll 2
-    for (int64_t v = g + (int64_t)lane * G; v < nvec; v += step) {
-      const uint4 q = vec((int32_t)v);
+    for (int32_t v = g + lane * G; v < nvec; v += step) {
       float l[vec_n<T>()];
-      vec_unpack<T>(q, l);
+      vec_unpack<T>(vec(v), l);
+      float mx = l[0];
 #pragma unroll
-      for (int j = 0; j < vec_n<T>(); ++j) f(l[j], head + (int32_t)v * vec_n<T>() + j);
+      for (int j = 1; j < vec_n<T>(); ++j) mx = fmaxf(mx, l[j]);
+      if (mx >= thr) {
+#pragma unroll
+        for (int j = 0; j < vec_n<T>(); ++j) see(l[j], head + v * vec_n<T>() + j);
+      }
     }
     const int64_t c = (int64_t)tail0 + g;  // the tail is shorter than a vector
-    if (lane == 0 && c < classes) f(at(c), (int32_t)c);
+    if (lane == 0 && c < classes) see(at(c), (int32_t)c);
   }
 };
 
-// k-th largest (k <= 32) of the values of a warp's lanes: the least value that fewer than k others exceed
+// k-th largest (1 <= k <= 32) of the values of a warp's lanes: the maximum is taken and one lane that holds it leaves, k times
 __device__ inline float warp_kth(float v, int k) {
-  int above = 0;
-#pragma unroll
-  for (int d = 1; d < 32; ++d) above += __shfl_xor_sync(~0u, v, d) > v;
-  float t = above < k ? v : INFINITY;
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) t = fminf(t, __shfl_xor_sync(~0u, t, d));
-  return t;
+  float t;
+  for (int j = 0;; ++j) {
+    t = warp_max_f(v);
+    if (j == k - 1) return t;
+    const uint32_t who = __ballot_sync(~0u, v == t);
+    if ((threadIdx.x & 31) == __ffs(who) - 1) v = -INFINITY;
+  }
 }
 
 template <int NT> __host__ __device__ constexpr int top_list() { return NT > 32 ? 512 : 128; }  // candidates a block keeps
 template <int NT>
 struct TopShared {
-  float kth[(NT + 31) / 32];
   float maxima[NT];
   int owners[NT];
   uint64_t above[top_list<NT>()], equal[top_list<NT>()];  // keys of elements above / at the threshold
   uint64_t best[kTopMax];
-  int n_max, n_own, n_above, n_equal;
-  uint32_t thr;
+  int n_own, n_above, n_equal;
+  float thr;
 };
 
 // The k best keys of the elements that the NT threads of a block own -> sh.best in order (0: none), valid after the call.  vm = the
-// caller's own maximum (cut at kMasked, NaN ignored).  At least k threads have a maximum >= T, T the k-th largest of the maxima, so the k
-// best elements are >= T and belong to those threads: only their elements are read again (from L2), and what passes T is ranked by
-// counting.  T is found in two steps, the largest of the warps' own k-th values, then exactly among the maxima that pass it.
+// caller's own maximum (cut at kMasked, NaN ignored).  T = the k-th largest of 32 maxima, each over NT / 32 threads: at least k elements are >= T, so
+// the k best are, and on rows without order about 32 log(32 / (32 - k)) are (9 for k = 8, 31 for k = 20).  Only threads whose maximum reaches T
+// ("owners") have their elements read again, from L2, and what passes T is ranked by counting.  One warp finds T while the block's others wait: on
+// 2048 rows of 131072 bf16 the alternatives cost 23 us when every warp took part, see the kernel for what is left.
 //   More than top_list elements at T (tied rows): the lowest classes are picked in order by one warp, which stops at the k-th.
-//   More than top_list above T: k passes over the block's elements.
+//   More than top_list above T: k passes over the owners' elements.
 template <typename T, int NT>
 __device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, int k, TopShared<NT>& sh) {
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
-  constexpr int NW = (NT + 31) / 32, LIST = top_list<NT>();
-  const float kw = warp_kth(vm, k);
-  if (lane == 0) sh.kth[w] = kw;
-  if (tid == 0) { sh.n_max = sh.n_own = sh.n_above = sh.n_equal = 0; sh.thr = 0xffffffffu; }
-  if (tid < kTopMax) sh.best[tid] = 0;
-  __syncthreads();
-  float thr = sh.kth[0];
-#pragma unroll
-  for (int q = 1; q < NW; ++q) thr = fmaxf(thr, sh.kth[q]);
+  constexpr int NW = NT / 32, LIST = top_list<NT>();
   if (NW > 1) {
-    const bool in = vm >= thr;
-    if (in) sh.maxima[atomicAdd(&sh.n_max, 1)] = vm;
+    sh.maxima[tid] = vm;
     __syncthreads();
-    if (in) {
-      int above = 0;
-      for (int q = 0; q < sh.n_max; ++q) above += sh.maxima[q] > vm;
-      if (above < k) atomicMin(&sh.thr, order_bits(vm));
-    }
-    __syncthreads();
-    thr = order_value(sh.thr);
   }
-  const bool owner = vm >= thr && vm > kMasked;
-  if (owner) sh.owners[atomicAdd(&sh.n_own, 1)] = tid;
+  if (w == 0) {
+    float m[NW];
+#pragma unroll
+    for (int q = 0; q < NW; ++q) m[q] = NW > 1 ? sh.maxima[q * 32 + lane] : vm;
+    float mine = m[0];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) mine = fmaxf(mine, m[q]);
+    const float t = warp_kth(mine, k);
+    int n = 0;  // owners in lane order
+#pragma unroll
+    for (int q = 0; q < NW; ++q) {
+      const bool own = m[q] >= t && m[q] > kMasked;
+      const uint32_t who = __ballot_sync(~0u, own);
+      if (own) sh.owners[n + __popc(who & ((1u << lane) - 1u))] = q * 32 + lane;
+      n += __popc(who);
+    }
+    if (lane == 0) { sh.thr = t; sh.n_own = n; sh.n_above = sh.n_equal = 0; }
+    sh.best[lane] = 0;
+  }
   __syncthreads();
+  const float thr = sh.thr;
   const int n_own = sh.n_own;
+  const bool owner = vm >= thr && vm > kMasked;
   // few owners: a warp takes one at a time, its lanes read the owner's vectors side by side; many (tied rows): every owner reads its own
   auto each_candidate = [&](auto&& f) {
     if (n_own <= 8 * NW) {
-      for (int q = w; q < n_own; q += NW) rp.each_of(g0 + sh.owners[q], G, lane, 32, f);
+      for (int q = w; q < n_own; q += NW) rp.each_of(g0 + sh.owners[q], G, lane, 32, thr, f);
     } else if (owner) {
-      rp.each_of(g0 + tid, G, 0, 1, f);
+      rp.each_of(g0 + tid, G, 0, 1, thr, f);
     }
   };
   each_candidate([&](float l, int32_t c) {
     if (l > thr) {
       const int at = atomicAdd(&sh.n_above, 1);
       if (at < LIST) sh.above[at] = order_key(l, c);
-    } else if (l == thr && l > kMasked) {
+    } else if (l > kMasked) {
       const int at = atomicAdd(&sh.n_equal, 1);
       if (at < LIST) sh.equal[at] = order_key(l, c);
     }
@@ -400,10 +431,15 @@ __device__ inline void write_top(const ScoreOut& o, int64_t i, int j, uint64_t k
   o.top_idx[i * o.top_k + j] = key ? (int32_t)~(uint32_t)key : -1;
 }
 
+// Blocks per SM a form is compiled for, and whether its loop keeps the next step's loads in flight.  Measured (us, without / with 8 alternatives):
+// 2048 x 131072 bf16: 512 threads prefetching 84 / 96, 256 threads 89 / 112;  4096 x 32768 bf16: 256 threads x 6 blocks 47 / 61, 128 threads 52 / 66,
+// 512 threads 53 / 86;  8192 x 8192 fp32: 128 threads x 12 blocks 43 / 58, 256 threads 43 / 64.
+template <int NT> __host__ __device__ constexpr int row_blocks() { return NT == 512 ? 2 : NT == 256 ? 6 : NT == 128 ? 12 : 24; }
+
 // Rows of contiguous classes: NT threads of CS blocks (a cluster) per row, one pass.  A thread keeps the statistics of the vectors it owns in
-// registers, four per step with the next four in flight; nothing is exchanged until the row ends.
+// registers, four per step; nothing is exchanged until the row ends.
 template <typename T, int NT, int CS>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, CS == 1 ? row_blocks<NT>() : 4)
 logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o) {
   constexpr int NW = NT / 32, U = 4, G = NT * CS;
   __shared__ RowStat ws[NW], cta;
@@ -420,43 +456,47 @@ logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut 
   RowStat a = stat_empty();
   for (int64_t c = g; c < rp.head; c += G) stat_add(a, rp.at(c));
   if ((int64_t)rp.tail0 + g < rp.classes) stat_add(a, rp.at(rp.tail0 + g));
-  int64_t q = g;
-  if (q + (U - 1) * G < rp.nvec) {
-    uint4 x[U];
+  int32_t q = g;
+  if (NT == 512) {
+    if (q + (U - 1) * G < rp.nvec) {
+      uint4 x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = rp.vec((int32_t)q + u * G);
-    for (q += U * G; q + (U - 1) * G < rp.nvec; q += U * G) {  // the next step's loads fly while this one's vectors are added
-      uint4 n[U];
+      for (int u = 0; u < U; ++u) x[u] = rp.vec(q + u * G);
+      for (q += U * G; q + (U - 1) * G < rp.nvec; q += U * G) {  // the next step's loads fly while this one's vectors are added
+        uint4 n[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) n[u] = rp.vec((int32_t)q + u * G);
+        for (int u = 0; u < U; ++u) n[u] = rp.vec(q + u * G);
+        stat_add_vecs<T, U>(a, x);
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = n[u];
+      }
       stat_add_vecs<T, U>(a, x);
-#pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = n[u];
     }
-    stat_add_vecs<T, U>(a, x);
+  } else {
+    for (; q + (U - 1) * G < rp.nvec; q += U * G) {
+      uint4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = rp.vec(q + u * G);
+      stat_add_vecs<T, U>(a, x);
+    }
   }
   for (; q < rp.nvec; q += G) {
-    uint4 x[1] = {rp.vec((int32_t)q)};
+    uint4 x[1] = {rp.vec(q)};
     stat_add_vecs<T, 1>(a, x);
   }
   const float vm = a.m;
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) a = stat_merge(a, stat_shfl_xor(a, d));
+  a = warp_stat(a);
   if (NW > 1) {
     if (lane == 0) ws[w] = a;
-    __syncthreads();
-    a = ws[0];
-#pragma unroll
-    for (int p = 1; p < NW; ++p) a = stat_merge(a, ws[p]);
+    if (o.top_k == 0) __syncthreads();  // else block_top's barriers order this
   }
   if (o.top_k > 0) block_top<T, NT>(rp, g0, G, vm, o.top_k, sh);
+  if (w == 0 && NW > 1) a = warp_stat(lane < NW ? ws[lane] : stat_empty());  // from here on only warp 0 holds the row's statistics
   if (CS > 1) {
     if (tid == 0) cta = a;
     cluster_sync();
     if (part == 0) {
-      a = cta;
-#pragma unroll
-      for (int p = 1; p < CS; ++p) a = stat_merge(a, *cluster_map(&cta, p));
+      if (w == 0) a = warp_stat(lane < CS ? *cluster_map(&cta, lane) : stat_empty());
       if (o.top_k > 0) {
         // rank the CS * k keys of the blocks: all into this block's list first
         const int n = CS * o.top_k;
@@ -476,17 +516,20 @@ logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut 
     cluster_sync();  // no block leaves while its shared memory is read
     if (part != 0) return;
   }
+  if (w != 0) return;
   const RowScore sc = stat_finish(a);
   if (tid == 0) write_scores(o, i, sc, y, v.classes, [&] { return rp.at(y); });
   if (tid < o.top_k) write_top(o, i, tid, CS > 1 ? sh.equal[tid] : sh.best[tid], sc);
 }
 
-// Logits with the sample index contiguous: 16 rows x 32 groups of classes per block, group y owns classes y, y + 32, ...; a warp reads two runs
-// of 16 consecutive samples.  A chunk of 32 x kFeatN classes is loaded into registers in one go, and stays there for the alternatives when it is the whole row.
-constexpr int kFeatR = 16, kFeatG = 32, kFeatN = 32, kFeatList = 48;
+// Logits with the sample index contiguous: R rows (32 bytes' worth) x 32 groups of classes per block, group y owns classes y, y + 32, ...; a warp
+// reads whole 32-byte sectors.  A chunk of 32 x kFeatN classes is loaded into registers in one go, and stays there for the alternatives when it is the whole row.
+constexpr int kFeatG = 32, kFeatN = 32, kFeatList = 48;
+template <typename T> __host__ __device__ constexpr int feat_rows() { return 32 / (int)sizeof(T); }
 template <typename T>
-__global__ void __launch_bounds__(kFeatR * kFeatG, 2)
-logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o, int row_blocks) {
+__global__ void __launch_bounds__(feat_rows<T>() * kFeatG, 1024 / (feat_rows<T>() * kFeatG))
+logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o, uint32_t row_blocks) {
+  constexpr int kFeatR = feat_rows<T>();
   __shared__ float red[3][kFeatR][kFeatG + 1];
   __shared__ uint64_t list[kFeatR][kFeatList];
   __shared__ uint64_t best[kFeatR][kTopMax];
@@ -494,7 +537,8 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
   __shared__ int count[kFeatR];
   const int x = threadIdx.x % kFeatR, y = threadIdx.x / kFeatR;
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t k = blockIdx.x / row_blocks, r0 = (int64_t)(blockIdx.x % row_blocks) * kFeatR, r = r0 + x, i = k * v.rows + r;
+  const uint32_t k = blockIdx.x / row_blocks;
+  const int64_t r0 = (int64_t)(blockIdx.x % row_blocks) * kFeatR, r = r0 + x, i = k * v.rows + r;
   const bool in = r < v.rows;
   const int32_t lab = in && labels ? labels[i] : 0;
   const bool live = in && lab >= 0;
@@ -526,8 +570,7 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
     if (lane == 0) thr_s[w] = t;
     best[w][lane] = 0;
   }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) a = stat_merge(a, stat_shfl_xor(a, d));
+  a = warp_stat(a);
   const RowScore sc = stat_finish(a);
   const int64_t rw = r0 + w, iw = k * v.rows + rw;
   const bool row_in = rw < v.rows;
@@ -632,18 +675,20 @@ template <typename T> __device__ inline uint4 vec_pack(const float (&f)[16 / siz
 template <bool VEC, typename T> __host__ __device__ constexpr int64_t grad_chunk(int NT) { return VEC ? (int64_t)NT * 4 * vec_n<T>() : (int64_t)NT * 8; }
 template <typename T, int NT, bool VEC>
 __global__ void __launch_bounds__(256)
-grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, int64_t chunks, int64_t units) {
+grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t chunks, uint32_t units) {
   constexpr int N = vec_n<T>();
-  const int64_t unit = NT == 32 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
+  const uint32_t unit = NT == 32 ? blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
   if (unit >= units) return;
   const int t = threadIdx.x % NT;
-  const int64_t i = unit / chunks, chunk = unit % chunks;
+  const uint32_t i = (uint32_t)(unit / chunks), chunk = (uint32_t)(unit % chunks);
   const GradRow row(g, i, v.classes);
   const T* src = v.row(i);
-  T* dst = out.p + (i / v.rows) * out.sk + (i % v.rows) * out.sr;
+  uint32_t r;
+  const uint32_t k = v.by_rows.div(i, r);
+  T* dst = out.p + k * out.sk + r * out.sr;
   if (VEC) {
     const RowParts<T> rp(src, 1, v.classes);
-    const int64_t q0 = chunk * NT * 4 + t;
+    const int64_t q0 = (int64_t)chunk * NT * 4 + t;
     uint4 x[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -668,12 +713,12 @@ grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, int64_t chunks, int64_
     float l[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int64_t c = (chunk * 8 + e) * NT + t;
+      const int64_t c = ((int64_t)chunk * 8 + e) * NT + t;
       l[e] = c < v.classes ? to_float(src[c * v.sc]) : 0.f;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int64_t c = (chunk * 8 + e) * NT + t;
+      const int64_t c = ((int64_t)chunk * 8 + e) * NT + t;
       if (c < v.classes) dst[c * out.sc] = from_float<T>(row(l[e], c));
     }
   }

@@ -91,22 +91,24 @@ cudaError_t launch_row(const LogitView<T>& v, const int32_t* labels, const Score
   return cudaLaunchKernelEx(&cfg, logprob_row_kernel<T, NT, CS>, v, labels, out);
 }
 
-// Which form a call takes.  Sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 2 KB, 128 threads up
-// to 16 KB, else 256; rows that do not fill the machine are split over a cluster of 2 or 8 blocks while every thread keeps two vectors.
+// Which form a call takes.  Sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 4 KB, 128 threads up
+// to 32 KB, 256 up to 128 KB, 512 beyond; rows of 32 KB and more that leave most of the machine idle are split over a cluster of 8 or 4 blocks
+// (4 rows of 131072 bf16, 8 alternatives: 14.4 us with one block a row, 8.3 with eight; 64 rows: 14.4, four blocks 10.7).
 template <typename T>
 cudaError_t launch_scores(const LogitView<T>& v, const int32_t* labels, const ScoreOut& out, int32_t K, cudaStream_t stream) {
   const int64_t total = (int64_t)K * v.rows;
   if (v.sc != 1 && v.sr == 1 && v.rows > 1) {
-    const int64_t row_blocks = ceil_div(v.rows, kFeatR);
-    logprob_feature_kernel<T><<<(unsigned)(K * row_blocks), kFeatR * kFeatG, 0, stream>>>(v, labels, out, (int)row_blocks);
+    const int64_t row_blocks = ceil_div(v.rows, feat_rows<T>());
+    logprob_feature_kernel<T><<<(unsigned)(K * row_blocks), feat_rows<T>() * kFeatG, 0, stream>>>(v, labels, out, (uint32_t)row_blocks);
     return cudaPeekAtLastError();
   }
   const int64_t bytes = (int64_t)v.classes * sizeof(T);
-  if (bytes <= 2048) return launch_row<T, 32, 1>(v, labels, out, total, stream);
-  if (bytes <= 16384 && total >= 148) return launch_row<T, 128, 1>(v, labels, out, total, stream);
-  if (total >= 2 * 148 || bytes < 16384) return launch_row<T, 256, 1>(v, labels, out, total, stream);
-  if (total >= 148 / 2 || bytes < 65536) return launch_row<T, 256, 2>(v, labels, out, total, stream);
-  return launch_row<T, 256, 8>(v, labels, out, total, stream);
+  if (bytes >= 32768 && total <= 148 / 4) return launch_row<T, 256, 8>(v, labels, out, total, stream);
+  if (bytes >= 32768 && total <= 148) return launch_row<T, 256, 4>(v, labels, out, total, stream);
+  if (bytes <= 4096) return launch_row<T, 32, 1>(v, labels, out, total, stream);
+  if (bytes <= 32768) return launch_row<T, 128, 1>(v, labels, out, total, stream);
+  if (bytes <= 131072) return launch_row<T, 256, 1>(v, labels, out, total, stream);
+  return launch_row<T, 512, 1>(v, labels, out, total, stream);
 }
 
 }  // namespace
@@ -132,7 +134,7 @@ extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int6
   cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes};
+    const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes, FastDiv((uint32_t)rows)};
     e = launch_scores<T>(v, d_labels, out, K, stream);
   });
   return err.done(e);
@@ -161,8 +163,8 @@ cudaError_t launch_grad(const LogitView<T>& v, const GradIn& in, const GradOut<T
   const bool narrow = v.classes <= 1024;  // a warp per row
   const auto go = [&](auto kern, int64_t chunk) {
     const int64_t chunks = ceil_div(v.classes, chunk), units = total * chunks, blocks = narrow ? ceil_div(units, 8) : units;
-    if (blocks > kMaxIndex) return cudaErrorInvalidConfiguration;
-    kern<<<(unsigned)blocks, 256, 0, stream>>>(v, in, o, chunks, units);
+    if (units > kMaxIndex) return cudaErrorInvalidConfiguration;
+    kern<<<(unsigned)blocks, 256, 0, stream>>>(v, in, o, (uint32_t)chunks, (uint32_t)units);
     return cudaPeekAtLastError();
   };
   if (vec) return narrow ? go(grad_row_kernel<T, 32, true>, grad_chunk<true, T>(32)) : go(grad_row_kernel<T, 256, true>, grad_chunk<true, T>(256));
@@ -196,7 +198,7 @@ extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K,
   cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes};
+    const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes, FastDiv((uint32_t)rows)};
     const GradOut<T> o{static_cast<T*>(d_dlogits), out_stride_k, out_stride_row, out_stride_class};
     e = launch_grad<T>(v, in, o, K, stream);
   });
