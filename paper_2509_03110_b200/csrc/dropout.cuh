@@ -16,7 +16,7 @@ struct DropArgs {
   uint32_t limit;                   // an element is dropped when its 16 bits, moved to the top of a word, are below `limit`
   bool some;                        // false: everything is dropped
   float scale;                      // 65536 / (65536 - cut)
-  FastDiv by_groups, by_rows;
+  FastDiv by_groups, by_rows;       // by_groups: groups of 8 (vector form) or segments of 256 columns per row
   __device__ inline void bits(uint32_t k, uint32_t r, uint32_t g, uint32_t (&w)[4]) const {  // columns 8 g .. 8 g + 7
     philox4x32_10(g, r, word2 + k, tick, key0, key1, w);
   }
@@ -85,34 +85,35 @@ dropout_vec_kernel(const T* x, const T* skip, T* out, DropArgs a, uint32_t total
 // consecutive lanes move consecutive elements.
 template <typename T>
 __global__ void __launch_bounds__(256)
-dropout_elem_kernel(const T* x, const T* skip, T* out, DropArgs a, int64_t segments, int64_t total) {
+dropout_elem_kernel(const T* x, const T* skip, T* out, DropArgs a, uint32_t total) {
   __shared__ __align__(16) uint16_t num[8][256];
   const int wp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * 8 + wp;
+  const uint32_t unit = blockIdx.x * 8 + wp;
   if (unit >= total) return;
-  const int64_t seg = unit % segments, kr = unit / segments, r = kr % a.rows, k = kr / a.rows, c0 = seg * 256 + lane;
-  const T* xp = x + k * a.xk + r * a.xr;
-  const T* sp = skip ? skip + k * a.sk + r * a.sr : nullptr;
-  T* op = out + k * a.ok + r * a.orr;
+  uint32_t seg, r;
+  const uint32_t k = a.by_rows.div(a.by_groups.div(unit, seg), r);
+  const int64_t c0 = (int64_t)seg * 256 + lane;
+  const int n = c0 < a.n ? (int)min((int64_t)8, (a.n - c0 + 31) / 32) : 0;  // this lane's columns
+  const T* xp = x + k * a.xk + r * a.xr + c0;
+  const T* sp = skip ? skip + k * a.sk + r * a.sr + c0 : nullptr;
+  T* op = out + k * a.ok + r * a.orr + c0;
   float v[8], s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const bool in = c0 + e * 32 < a.n;
-    v[e] = in ? to_float(xp[c0 + e * 32]) : 0.f;
-    s[e] = in && sp ? to_float(sp[c0 + e * 32]) : 0.f;
+    v[e] = e < n ? to_float(xp[e * 32]) : 0.f;
+    s[e] = e < n && sp ? to_float(sp[e * 32]) : 0.f;
   }
   uint32_t w[4];
-  a.bits((uint32_t)k, (uint32_t)r, (uint32_t)(seg * 32 + lane), w);
+  a.bits(k, r, seg * 32 + lane, w);
   *reinterpret_cast<uint4*>(&num[wp][lane * 8]) = make_uint4(w[0], w[1], w[2], w[3]);
   __syncwarp();
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int64_t c = c0 + e * 32;
-    if (c >= a.n) break;
-    float y = a.value(v[e], (uint32_t)num[wp][lane + e * 32] << 16);
-    if (sp) y += s[e];
-    op[c] = from_float<T>(y);
-  }
+  for (int e = 0; e < 8; ++e)
+    if (e < n) {
+      float y = a.value(v[e], (uint32_t)num[wp][lane + e * 32] << 16);
+      if (sp) y += s[e];
+      op[e * 32] = from_float<T>(y);
+    }
 }
 
 }  // namespace lsam

@@ -25,6 +25,7 @@ __device__ inline float ex2(float x) {
 // logits costs no digits of the entropy or of a log probability.  Logits at or below kMasked are masks: they enter as kMasked, whose 2^w is 0
 // beside any other (and (-inf) * 0 never arises); a set of nothing but masks has m = kMasked.  A NaN or +inf logit makes s NaN.
 constexpr float kMasked = -1e30f;
+__device__ inline float above_masked() { return __uint_as_float(__float_as_uint(kMasked) - 1u); }  // the least fp32 number above it
 struct RowStat { float m, s, t; };
 __device__ inline float max_nan(float a, float b) {  // NaN if either is
   float y;
@@ -176,27 +177,44 @@ __device__ inline void stat_add_all(RowStat& a, const float (&l)[N], float mx) {
   unpack2(t2, x, y);
   a.t += x + y;
 }
-// Cuts U vectors at kMasked, takes their maximum and adds them.
+// Cuts U vectors at kMasked and adds them; returns their maximum.
 template <typename T, int U>
-__device__ inline void stat_add_vecs(RowStat& a, uint4 (&q)[U]) {
+__device__ inline float stat_add_vecs(RowStat& a, uint4 (&q)[U]) {
   constexpr int N = vec_n<T>();
   float mx = kMasked, l[U * N];
-  if constexpr (std::is_same<T, bf16>::value) {
-    // bf16: cut and compared in pairs; the bound is the bf16 next below kMasked
-    constexpr uint32_t cut = 0xf14af14au;
-    uint32_t m2 = cut;
+  if constexpr (sizeof(T) == 2) {
+    // 16-bit logits are compared in pairs; until their exponentials they stay packed (held as floats, a step of fp16 would not leave room for five
+    // blocks).  bf16 is cut in pairs too, at the bf16 next below kMasked; fp16 has no such number and is cut after the conversion.
+    constexpr bool BF = std::is_same<T, bf16>::value;
+    uint32_t m2 = BF ? 0xf14af14au : 0xfc00fc00u;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+      uint32_t* w = reinterpret_cast<uint32_t*>(&q[u]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w[j]) : "r"(w[j]), "r"(cut));
-        asm("max.bf16x2 %0, %1, %2;" : "=r"(m2) : "r"(m2), "r"(w[j]));
-        l[u * 8 + 2 * j] = __uint_as_float(w[j] << 16);
-        l[u * 8 + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        if (BF) {
+          asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w[j]) : "r"(w[j]), "r"(0xf14af14au));
+          asm("max.bf16x2 %0, %1, %2;" : "=r"(m2) : "r"(m2), "r"(w[j]));
+        } else {
+          asm("max.f16x2 %0, %1, %2;" : "=r"(m2) : "r"(m2), "r"(w[j]));
+        }
       }
     }
-    mx = fmaxf(mx, fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xffff0000u)));
+    float top[2];
+    if (BF) {
+      top[0] = __uint_as_float(m2 << 16); top[1] = __uint_as_float(m2 & 0xffff0000u);
+    } else {
+      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&m2));
+      top[0] = t.x; top[1] = t.y;
+    }
+    mx = fmaxf(mx, fmaxf(top[0], top[1]));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[N];
+      vec_unpack<T>(q[u], f);
+#pragma unroll
+      for (int j = 0; j < N; ++j) l[u * N + j] = BF ? f[j] : max_nan(f[j], kMasked);
+    }
   } else {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -210,6 +228,7 @@ __device__ inline void stat_add_vecs(RowStat& a, uint4 (&q)[U]) {
     }
   }
   stat_add_all(a, l, mx);
+  return mx;
 }
 
 __device__ inline void cluster_sync() {
@@ -265,23 +284,43 @@ struct RowParts {
   }
 };
 
-// k-th largest (1 <= k <= 32) of the values of a warp's lanes: the maximum is taken and one lane that holds it leaves, k times
+// k-th largest (1 <= k <= 32) of the values of a warp's lanes.  Small k: the maximum is taken and one lane that holds it leaves, k times; else the
+// least value that fewer than k others exceed (31 independent exchanges instead of k dependent steps).
 __device__ inline float warp_kth(float v, int k) {
   float t;
-  for (int j = 0;; ++j) {
-    t = warp_max_f(v);
-    if (j == k - 1) return t;
-    const uint32_t who = __ballot_sync(~0u, v == t);
-    if ((threadIdx.x & 31) == __ffs(who) - 1) v = -INFINITY;
+  if (k <= 4) {
+    for (int j = 0;; ++j) {
+      t = warp_max_f(v);
+      if (j == k - 1) return t;
+      const uint32_t who = __ballot_sync(~0u, v == t);
+      if ((threadIdx.x & 31) == __ffs(who) - 1) v = -INFINITY;
+    }
   }
+  int above = 0;
+#pragma unroll
+  for (int d = 1; d < 32; ++d) above += __shfl_xor_sync(~0u, v, d) > v;
+  const float low = above < k ? v : INFINITY;
+  asm("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(t) : "f"(low));
+  return t;
 }
 
-template <int NT> __host__ __device__ constexpr int top_list() { return NT > 32 ? 512 : 128; }  // candidates a block keeps
+constexpr int kTopList = 512;  // candidates a block keeps
+// What a thread knows of its own elements: the first vector of the step that holds its maximum (-1: a scalar does) and the maximum of all others.
+struct StepMax {
+  int32_t step = -1;
+  float second = kMasked;
+  __device__ inline void see(float before, float mx, int32_t q) {
+    if (mx > before) { second = before; step = q; }
+    else second = fmaxf(second, mx);
+  }
+};
+constexpr int kStep = 4;  // vectors a thread takes per step
 template <int NT>
 struct TopShared {
-  float maxima[NT];
+  float maxima[NT], second[NT];
+  int32_t step[NT];
   int owners[NT];
-  uint64_t above[top_list<NT>()], equal[top_list<NT>()];  // keys of elements above / at the threshold
+  uint64_t above[kTopList], equal[kTopList];  // keys of elements above / at the threshold
   uint64_t best[kTopMax];
   int n_own, n_above, n_equal;
   float thr;
@@ -290,22 +329,22 @@ struct TopShared {
 // The k best keys of the elements that the NT threads of a block own -> sh.best in order (0: none), valid after the call.  vm = the
 // caller's own maximum (cut at kMasked, NaN ignored).  T = the k-th largest of 32 maxima, each over NT / 32 threads: at least k elements are >= T, so
 // the k best are, and on rows without order about 32 log(32 / (32 - k)) are (9 for k = 8, 31 for k = 20).  Only threads whose maximum reaches T
-// ("owners") have their elements read again, from L2, and what passes T is ranked by counting.  One warp finds T while the block's others wait: on
-// 2048 rows of 131072 bf16 the alternatives cost 23 us when every warp took part, see the kernel for what is left.
-//   More than top_list elements at T (tied rows): the lowest classes are picked in order by one warp, which stops at the k-th.
-//   More than top_list above T: k passes over the owners' elements.
+// ("owners") have elements read again, the step that holds the maximum (64 bytes), or all of them where another step reaches T too; what
+// passes T is ranked by counting.  (A row of 256 KB has partly left L2 by then: reading all of an owner's elements again cost 17 us per 2048 rows.)
+//   More than kTopList elements at T (tied rows): the lowest classes are picked in order by one warp, which stops at the k-th.
+//   More than kTopList above T: k passes over the owners' elements.
 template <typename T, int NT>
-__device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, int k, TopShared<NT>& sh) {
+__device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, const StepMax& sm, int k, TopShared<NT>& sh) {
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
-  constexpr int NW = NT / 32, LIST = top_list<NT>();
-  if (NW > 1) {
-    sh.maxima[tid] = vm;
-    __syncthreads();
-  }
+  constexpr int NW = NT / 32, LIST = kTopList, U = kStep;
+  sh.maxima[tid] = vm;
+  sh.second[tid] = sm.second;
+  sh.step[tid] = sm.step;
+  __syncthreads();
   if (w == 0) {
     float m[NW];
 #pragma unroll
-    for (int q = 0; q < NW; ++q) m[q] = NW > 1 ? sh.maxima[q * 32 + lane] : vm;
+    for (int q = 0; q < NW; ++q) m[q] = sh.maxima[q * 32 + lane];
     float mine = m[0];
 #pragma unroll
     for (int q = 1; q < NW; ++q) mine = fmaxf(mine, m[q]);
@@ -325,23 +364,38 @@ __device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, int k,
   const float thr = sh.thr;
   const int n_own = sh.n_own;
   const bool owner = vm >= thr && vm > kMasked;
-  // few owners: a warp takes one at a time, its lanes read the owner's vectors side by side; many (tied rows): every owner reads its own
-  auto each_candidate = [&](auto&& f) {
+  // all elements of the owners that `which` names: few owners, a warp takes one at a time, its lanes read the owner's vectors side by side;
+  // many (tied rows), every owner reads its own
+  auto each_candidate = [&](auto&& f, auto&& which) {
     if (n_own <= 8 * NW) {
-      for (int q = w; q < n_own; q += NW) rp.each_of(g0 + sh.owners[q], G, lane, 32, thr, f);
-    } else if (owner) {
+      for (int q = w; q < n_own; q += NW)
+        if (which(sh.owners[q])) rp.each_of(g0 + sh.owners[q], G, lane, 32, thr, f);
+    } else if (owner && which(tid)) {
       rp.each_of(g0 + tid, G, 0, 1, thr, f);
     }
   };
-  each_candidate([&](float l, int32_t c) {
+  auto offer = [&](float l, int32_t c) {
     if (l > thr) {
       const int at = atomicAdd(&sh.n_above, 1);
       if (at < LIST) sh.above[at] = order_key(l, c);
-    } else if (l > kMasked) {
+    } else if (l == thr && l > kMasked) {
       const int at = atomicAdd(&sh.n_equal, 1);
       if (at < LIST) sh.equal[at] = order_key(l, c);
     }
-  });
+  };
+  for (int e = tid; e < n_own * U; e += NT) {
+    const int own = sh.owners[e / U], u = e % U;
+    const int32_t q = sh.step[own];
+    if (q >= 0 && sh.second[own] < thr && (u == 0 || q + (U - 1) * G < rp.nvec)) {  // the row's last vectors are steps of one
+      const int32_t v = q + u * G;
+      float l[vec_n<T>()];
+      vec_unpack<T>(rp.vec(v), l);
+#pragma unroll
+      for (int j = 0; j < vec_n<T>(); ++j)
+        if (l[j] >= thr) offer(l[j], rp.head + v * vec_n<T>() + j);
+    }
+  }
+  each_candidate(offer, [&](int own) { return sh.step[own] < 0 || sh.second[own] >= thr; });
   __syncthreads();
   const int na = sh.n_above, ne = sh.n_equal;
   if (na > LIST) {
@@ -352,7 +406,7 @@ __device__ void block_top(const RowParts<T>& rp, int g0, int G, float vm, int k,
         const uint64_t key = order_key(l, c);
         if (key < last && key > best) best = key;
       };
-      each_candidate(see);
+      each_candidate(see, [](int) { return true; });
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) best = max(best, (uint64_t)__shfl_xor_sync(~0u, (unsigned long long)best, d));
       __syncthreads();
@@ -420,9 +474,8 @@ __device__ inline void write_left_out(const ScoreOut& o, int64_t i) {
   if (o.entropy) o.entropy[i] = 0.f;
   write_no_top(o, i, 0);
 }
-template <typename L>
-__device__ inline void write_scores(const ScoreOut& o, int64_t i, const RowScore& sc, int32_t y, int32_t classes, L&& label_logit) {
-  if (o.logp) o.logp[i] = y < classes ? score_logp(label_logit(), sc) : NAN;
+__device__ inline void write_scores(const ScoreOut& o, int64_t i, const RowScore& sc, int32_t y, int32_t classes, float at_label) {
+  if (o.logp) o.logp[i] = y < classes ? score_logp(at_label, sc) : NAN;
   if (o.lse) o.lse[i] = sc.lse;
   if (o.entropy) o.entropy[i] = sc.ent;
 }
@@ -431,20 +484,127 @@ __device__ inline void write_top(const ScoreOut& o, int64_t i, int j, uint64_t k
   o.top_idx[i * o.top_k + j] = key ? (int32_t)~(uint32_t)key : -1;
 }
 
-// Blocks per SM a form is compiled for, and whether its loop keeps the next step's loads in flight.  Measured (us, without / with 8 alternatives):
-// 2048 x 131072 bf16: 512 threads prefetching 84 / 96, 256 threads 89 / 112;  4096 x 32768 bf16: 256 threads x 6 blocks 47 / 61, 128 threads 52 / 66,
-// 512 threads 53 / 86;  8192 x 8192 fp32: 128 threads x 12 blocks 43 / 58, 256 threads 43 / 64.
-template <int NT> __host__ __device__ constexpr int row_blocks() { return NT == 512 ? 2 : NT == 256 ? 6 : NT == 128 ? 12 : 24; }
+// The alternatives of a row whose 32 x n elements sit in the registers of one warp: the k best keys -> best (shared memory, kTopMax), `list` its candidate
+// list.  thr: at least k elements reach it.  key(j): the caller's j-th key (0: no alternative).
+template <int N, class F>
+__device__ inline void warp_top(float thr, const float (&l)[N], int k, uint64_t* list, int list_n, int* count, uint64_t* best, F&& class_of) {
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) *count = 0;
+  best[lane] = 0;
+  const float least = fmaxf(thr, above_masked());
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (l[j] >= least) {
+      const int at = atomicAdd(count, 1);
+      if (at < list_n) list[at] = order_key(l[j], class_of(j));
+    }
+  __syncwarp();
+  const int n = *count;
+  if (n <= list_n) {
+    for (int q = lane; q < n; q += 32) {
+      const uint64_t key = list[q];
+      int r = 0;
+      for (int z = 0; z < n; ++z) r += list[z] > key;
+      if (r < k) best[r] = key;
+    }
+  } else {
+    // more candidates than the list holds (ties): the best key below the previous one, k times
+    uint64_t last = ~0ull;
+    for (int j = 0; j < k; ++j) {
+      uint64_t b = 0;
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        const uint64_t key = order_key(l[q], class_of(q));
+        if (key < last && key > b) b = key;
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) b = max(b, (uint64_t)__shfl_xor_sync(~0u, (unsigned long long)b, d));
+      if (lane == 0) best[j] = b;
+      last = b;
+    }
+  }
+  __syncwarp();
+}
 
-// Rows of contiguous classes: NT threads of CS blocks (a cluster) per row, one pass.  A thread keeps the statistics of the vectors it owns in
-// registers, four per step; nothing is exchanged until the row ends.
+// Rows of at most 1024 classes: a warp per row, 32 logits a lane in registers, so that the maximum is known before the first exponential and the
+// alternatives cost no second read.  VEC: every row starts on a 16-byte boundary.
+constexpr int kWarpClasses = 1024, kWarpList = 64;
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256)
+logprob_warp_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o, uint32_t total) {
+  __shared__ uint64_t list[8][kWarpList], best[8][kTopMax];
+  __shared__ int count[8];
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t i = blockIdx.x * 8 + w;
+  if (i >= total) return;
+  const int32_t y = labels ? labels[i] : 0;
+  if (y < 0) {
+    if (lane == 0) write_left_out(o, i);
+    return;
+  }
+  const T* row = v.row(i);
+  const float at_label = lane == 0 && o.logp && y < v.classes ? to_float(row[y * v.sc]) : NAN;
+  constexpr int N = vec_n<T>();
+  float l[32];
+  if (VEC) {
+    uint4 x[32 / N];
+    const int nvec = v.classes / N;
+#pragma unroll
+    for (int j = 0; j < 32 / N; ++j)
+      if (j * 32 + lane < nvec) x[j] = __ldg(reinterpret_cast<const uint4*>(row) + j * 32 + lane);
+#pragma unroll
+    for (int j = 0; j < 32 / N; ++j) {
+      float f[N];
+      if (j * 32 + lane < nvec) {
+        vec_unpack<T>(x[j], f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int c = (j * 32 + lane) * N + e;
+          f[e] = c < v.classes ? to_float(row[c]) : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) l[j * N + e] = f[e];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const int c = j * 32 + lane;
+      l[j] = c < v.classes ? to_float(row[c * v.sc]) : -INFINITY;
+    }
+  }
+  float mx = kMasked;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    l[j] = max_nan(l[j], kMasked);
+    mx = fmaxf(mx, l[j]);
+  }
+  RowStat a = {warp_max_f(mx), 0.f, 0.f};
+  stat_add_all(a, l, a.m);
+  a = warp_stat(a);
+  const RowScore sc = stat_finish(a);
+  if (lane == 0) write_scores(o, i, sc, y, v.classes, at_label);
+  if (o.top_k == 0) return;
+  warp_top(warp_kth(mx, o.top_k), l, o.top_k, list[w], kWarpList, &count[w], best[w], [&](int j) { return VEC ? (j / N * 32 + lane) * N + j % N : j * 32 + lane; });
+  if (lane < o.top_k) write_top(o, i, lane, best[w][lane], sc);
+}
+
+// Blocks per SM a form is compiled for.  Measured (us, without / with 8 alternatives): 2048 x 131072 bf16: 256 threads x 5 blocks 89 / 99, x 6 (spilling) 99 /
+// 110, 512 threads x 3 94 / 107;  4096 x 32768 bf16: 256 x 5 49 / 65, 128 threads x 10 51 / 64, 512 x 3 58 / 82;  8192 x 8192 fp32: 128 x 10 43 / 57,
+// 256 x 5 43 / 70.  A loop that kept the next step's loads in flight gained nothing over the blocks it cost.
+template <int NT, int CS> __host__ __device__ constexpr int row_blocks() { return CS > 1 ? 4 : NT == 256 ? 5 : 10; }
+
+// Rows of contiguous classes (or of any stride, one element at a time): NT threads of CS blocks (a cluster) per row, one pass.  A thread keeps the
+// statistics of the vectors it owns in registers, a step of them at a time; nothing is exchanged until the row ends.
 template <typename T, int NT, int CS>
-__global__ void __launch_bounds__(NT, CS == 1 ? row_blocks<NT>() : 4)
+__global__ void __launch_bounds__(NT, row_blocks<NT, CS>())
 logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o) {
-  constexpr int NW = NT / 32, U = 4, G = NT * CS;
+  constexpr int NW = NT / 32, U = kStep, G = NT * CS;
   __shared__ RowStat ws[NW], cta;
   __shared__ TopShared<NT> sh;
-  const int64_t i = blockIdx.x / CS;
+  const uint32_t i = blockIdx.x / CS;
   const int part = CS > 1 ? (int)(blockIdx.x % CS) : 0;
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g0 = part * NT, g = g0 + tid;
   const int32_t y = labels ? labels[i] : 0;
@@ -453,45 +613,30 @@ logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut 
     return;
   }
   const RowParts<T> rp(v.row(i), v.sc, v.classes);
+  const float at_label = g == 0 && o.logp && y < v.classes ? rp.at(y) : NAN;  // asked for now, needed when the row ends
   RowStat a = stat_empty();
   for (int64_t c = g; c < rp.head; c += G) stat_add(a, rp.at(c));
   if ((int64_t)rp.tail0 + g < rp.classes) stat_add(a, rp.at(rp.tail0 + g));
+  StepMax sm;
   int32_t q = g;
-  if (NT == 512) {
-    if (q + (U - 1) * G < rp.nvec) {
-      uint4 x[U];
+  for (; q + (U - 1) * G < rp.nvec; q += U * G) {
+    uint4 x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = rp.vec(q + u * G);
-      for (q += U * G; q + (U - 1) * G < rp.nvec; q += U * G) {  // the next step's loads fly while this one's vectors are added
-        uint4 n[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) n[u] = rp.vec(q + u * G);
-        stat_add_vecs<T, U>(a, x);
-#pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = n[u];
-      }
-      stat_add_vecs<T, U>(a, x);
-    }
-  } else {
-    for (; q + (U - 1) * G < rp.nvec; q += U * G) {
-      uint4 x[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = rp.vec(q + u * G);
-      stat_add_vecs<T, U>(a, x);
-    }
+    for (int u = 0; u < U; ++u) x[u] = rp.vec(q + u * G);
+    const float before = a.m;
+    sm.see(before, stat_add_vecs<T, U>(a, x), q);
   }
   for (; q < rp.nvec; q += G) {
     uint4 x[1] = {rp.vec(q)};
-    stat_add_vecs<T, 1>(a, x);
+    const float before = a.m;
+    sm.see(before, stat_add_vecs<T, 1>(a, x), q);
   }
   const float vm = a.m;
   a = warp_stat(a);
-  if (NW > 1) {
-    if (lane == 0) ws[w] = a;
-    if (o.top_k == 0) __syncthreads();  // else block_top's barriers order this
-  }
-  if (o.top_k > 0) block_top<T, NT>(rp, g0, G, vm, o.top_k, sh);
-  if (w == 0 && NW > 1) a = warp_stat(lane < NW ? ws[lane] : stat_empty());  // from here on only warp 0 holds the row's statistics
+  if (lane == 0) ws[w] = a;
+  if (o.top_k == 0) __syncthreads();  // else block_top's barriers order this
+  else block_top<T, NT>(rp, g0, G, vm, sm, o.top_k, sh);
+  if (w == 0) a = warp_stat(lane < NW ? ws[lane] : stat_empty());  // from here on only warp 0 holds the row's statistics
   if (CS > 1) {
     if (tid == 0) cta = a;
     cluster_sync();
@@ -501,7 +646,6 @@ logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut 
         // rank the CS * k keys of the blocks: all into this block's list first
         const int n = CS * o.top_k;
         for (int p = tid; p < n; p += NT) sh.above[p] = cluster_map(sh.best, p / o.top_k)[p % o.top_k];
-        __syncthreads();
         if (tid < kTopMax) sh.equal[tid] = 0;
         __syncthreads();
         for (int p = tid; p < n; p += NT) {
@@ -518,7 +662,7 @@ logprob_row_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut 
   }
   if (w != 0) return;
   const RowScore sc = stat_finish(a);
-  if (tid == 0) write_scores(o, i, sc, y, v.classes, [&] { return rp.at(y); });
+  if (tid == 0) write_scores(o, i, sc, y, v.classes, at_label);
   if (tid < o.top_k) write_top(o, i, tid, CS > 1 ? sh.equal[tid] : sh.best[tid], sc);
 }
 
@@ -543,15 +687,15 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
   const int32_t lab = in && labels ? labels[i] : 0;
   const bool live = in && lab >= 0;
   const T* p = v.p + k * v.sk + (live ? r : 0) * v.sr;
+  const int64_t step = kFeatG * v.sc;
   RowStat a = stat_empty();
   float l[kFeatN];
-  for (int64_t c0 = 0; c0 < v.classes; c0 += kFeatG * kFeatN) {
+  for (int64_t c0 = y; c0 < v.classes || c0 == y; c0 += kFeatG * kFeatN) {
     float mx = kMasked;
+    const int n = live ? (int)min((int64_t)kFeatN, (v.classes - c0 + kFeatG - 1) / kFeatG) : 0;  // this thread's classes of the chunk
+    const T* q = p + c0 * v.sc;
 #pragma unroll
-    for (int j = 0; j < kFeatN; ++j) {
-      const int64_t c = c0 + y + kFeatG * j;
-      l[j] = live && c < v.classes ? to_float(p[c * v.sc]) : -INFINITY;
-    }
+    for (int j = 0; j < kFeatN; ++j, q += step) l[j] = j < n ? to_float(*q) : -INFINITY;
 #pragma unroll
     for (int j = 0; j < kFeatN; ++j) {
       l[j] = max_nan(l[j], kMasked);
@@ -559,6 +703,12 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
     }
     stat_add_all(a, l, mx);
   }
+  // warp w ends row w; its label's logit is asked for before the block meets
+  const int64_t rw = r0 + w, iw = k * v.rows + rw;
+  const bool row_in = rw < v.rows;
+  const int32_t yw = row_in && labels ? labels[iw] : 0;
+  const T* pw = v.p + k * v.sk + (row_in ? rw : 0) * v.sr;
+  const float at_label = lane == 0 && row_in && o.logp && yw >= 0 && yw < v.classes ? to_float(pw[(int64_t)yw * v.sc]) : NAN;
   const float vm = a.m;
   red[0][x][y] = a.m; red[1][x][y] = a.s; red[2][x][y] = a.t;
   if (threadIdx.x < kFeatR) count[threadIdx.x] = 0;
@@ -572,24 +722,20 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
   }
   a = warp_stat(a);
   const RowScore sc = stat_finish(a);
-  const int64_t rw = r0 + w, iw = k * v.rows + rw;
-  const bool row_in = rw < v.rows;
-  const int32_t yw = row_in && labels ? labels[iw] : 0;
-  const T* pw = v.p + k * v.sk + (row_in ? rw : 0) * v.sr;
   if (lane == 0 && row_in) {
     if (yw < 0) write_left_out(o, iw);
-    else write_scores(o, iw, sc, yw, v.classes, [&] { return to_float(pw[(int64_t)yw * v.sc]); });
+    else write_scores(o, iw, sc, yw, v.classes, at_label);
   }
   if (o.top_k == 0) return;
   __syncthreads();
-  const float thr = thr_s[x];
+  const float least = fmaxf(thr_s[x], above_masked());
   auto offer = [&](float val, int64_t c) {
-    if (val >= thr && val > kMasked) {
+    if (val >= least) {
       const int at = atomicAdd(&count[x], 1);
       if (at < kFeatList) list[x][at] = order_key(val, (int32_t)c);
     }
   };
-  if (live && vm >= thr && vm > kMasked) {
+  if (live && vm >= least) {
     if (v.classes <= kFeatG * kFeatN) {
 #pragma unroll
       for (int j = 0; j < kFeatN; ++j) offer(l[j], y + kFeatG * j);
@@ -639,26 +785,25 @@ struct GradOut { T* p; int64_t sk, sr, sc; };
 
 struct GradRow {
   float lse, c0, c1, at_label;
-  int32_t y;   // class that receives at_label, -1: none
-  bool none;   // all zeros
-  __device__ inline GradRow() : lse(0.f), c0(0.f), c1(0.f), at_label(0.f), y(-1), none(true) {}
+  int32_t y;   // class that receives at_label, -1: none, -2: the whole row is zero
+  __device__ inline GradRow() : lse(0.f), c0(0.f), c1(0.f), at_label(0.f), y(-2) {}
   __device__ inline GradRow(const GradIn& g, int64_t i, int32_t classes) {
     y = g.labels ? g.labels[i] : -1;
     lse = g.lse[i];
-    none = (g.labels && y < 0) || lse == -INFINITY;
     const float a = g.dlogp ? g.dlogp[i] : 0.f;
     const float b = g.dentropy ? g.dentropy[i] : 0.f;
     c0 = -a - (g.dentropy ? b * g.entropy[i] : 0.f);
     c1 = -b;
     at_label = a;
+    if ((g.labels && y < 0) || lse == -INFINITY) y = -2;
     if (y >= classes) c0 = NAN;  // the whole row
   }
-  __device__ inline float operator()(float l, int64_t c) const {
+  __device__ inline float operator()(float l, int32_t c) const {
     const float u = max_nan(l - lse, -200.f);  // e^-200 is 0 in 32 bits, and (-inf) * 0 never arises
     const float p = ex2(u * kLog2e);
     float d = p * fmaf(c1, u, c0);
     if (c == y) d += at_label;
-    return none ? 0.f : d;
+    return y == -2 ? 0.f : d;
   }
 };
 
@@ -670,64 +815,67 @@ template <typename T> __device__ inline uint4 vec_pack(const float (&f)[16 / siz
   return q;
 }
 
-// Rows of contiguous classes.  NT = 256: a block takes a chunk of a row, 32: a warp does (eight rows per block).  VEC: input and output rows have the
-// same 16-byte phase (the host checks the strides), so that both move as vectors; else consecutive lanes move consecutive elements.
-template <bool VEC, typename T> __host__ __device__ constexpr int64_t grad_chunk(int NT) { return VEC ? (int64_t)NT * 4 * vec_n<T>() : (int64_t)NT * 8; }
-template <typename T, int NT, bool VEC>
+// Rows of classes.  NT = 256: a block takes a chunk of a row, 32: a warp does (eight rows per block).  VECTORS: input and output rows have the
+// same 16-byte phase (the host checks the strides), so that both move as vectors; UNIT: contiguous, consecutive lanes move consecutive elements; ANY: any stride.
+enum : int { GRAD_VECTORS = 0, GRAD_UNIT = 1, GRAD_ANY = 2 };
+template <typename T> __host__ __device__ constexpr int64_t grad_chunk(int mode, int NT) { return mode == GRAD_VECTORS ? (int64_t)NT * 4 * vec_n<T>() : (int64_t)NT * 8; }
+template <typename T, int NT, int MODE>
 __global__ void __launch_bounds__(256)
-grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t chunks, uint32_t units) {
+grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, FastDiv by_chunks, uint32_t units) {
   constexpr int N = vec_n<T>();
   const uint32_t unit = NT == 32 ? blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
   if (unit >= units) return;
   const int t = threadIdx.x % NT;
-  const uint32_t i = (uint32_t)(unit / chunks), chunk = (uint32_t)(unit % chunks);
-  const GradRow row(g, i, v.classes);
-  const T* src = v.row(i);
-  uint32_t r;
-  const uint32_t k = v.by_rows.div(i, r);
+  uint32_t chunk, r;
+  const uint32_t i = by_chunks.div(unit, chunk), k = v.by_rows.div(i, r);
+  const T* src = v.p + k * v.sk + r * v.sr;
   T* dst = out.p + k * out.sk + r * out.sr;
-  if (VEC) {
+  if (MODE == GRAD_VECTORS) {
     const RowParts<T> rp(src, 1, v.classes);
-    const int64_t q0 = (int64_t)chunk * NT * 4 + t;
+    const int32_t q0 = (int32_t)chunk * NT * 4 + t;
+    const uint4* from = reinterpret_cast<const uint4*>(src + rp.head) + q0;
+    uint4* to = reinterpret_cast<uint4*>(dst + rp.head) + q0;
     uint4 x[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (q0 + e * NT < rp.nvec) x[e] = reinterpret_cast<const uint4*>(src + rp.head)[q0 + e * NT];
+      if (q0 + e * NT < rp.nvec) x[e] = from[e * NT];
+    const GradRow row(g, i, v.classes);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int64_t q = q0 + e * NT;
-      if (q >= rp.nvec) break;
+      if (q0 + e * NT >= rp.nvec) break;
       float l[N];
       vec_unpack<T>(x[e], l);
-      const int64_t c = rp.head + q * N;
+      const int32_t c = rp.head + (q0 + e * NT) * N;
 #pragma unroll
       for (int j = 0; j < N; ++j) l[j] = row(l[j], c + j);
-      reinterpret_cast<uint4*>(dst + rp.head)[q] = vec_pack<T>(l);
+      to[e * NT] = vec_pack<T>(l);
     }
     if (chunk == 0) {  // both are shorter than a vector
       if (t < rp.head) dst[t] = from_float<T>(row(to_float(src[t]), t));
       const int64_t c = (int64_t)rp.tail0 + t;
-      if (c < v.classes) dst[c] = from_float<T>(row(to_float(src[c]), c));
+      if (c < v.classes) dst[c] = from_float<T>(row(to_float(src[c]), (int32_t)c));
     }
   } else {
-    float l[8];
+    const int64_t si = MODE == GRAD_UNIT ? 1 : v.sc, so = MODE == GRAD_UNIT ? 1 : out.sc;
+    const int64_t c0 = (int64_t)chunk * 8 * NT + t;
+    const int n = c0 < v.classes ? (int)min((int64_t)8, (v.classes - c0 + NT - 1) / NT) : 0;
+    const T* from = src + c0 * si;
+    T* to = dst + c0 * so;
+    T x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int64_t c = ((int64_t)chunk * 8 + e) * NT + t;
-      l[e] = c < v.classes ? to_float(src[c * v.sc]) : 0.f;
-    }
+    for (int e = 0; e < 8; ++e)
+      if (e < n) x[e] = from[e * NT * si];
+    const GradRow row(g, i, v.classes);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int64_t c = ((int64_t)chunk * 8 + e) * NT + t;
-      if (c < v.classes) dst[c * out.sc] = from_float<T>(row(l[e], c));
-    }
+    for (int e = 0; e < 8; ++e)
+      if (e < n) to[e * NT * so] = from_float<T>(row(to_float(x[e]), (int32_t)c0 + e * NT));
   }
 }
 
 // Logits and gradient with the sample index contiguous: a thread owns R consecutive rows (a 16-byte vector, or one row where the strides do
 // not allow it) and 8 classes of a block's 64.  block (32, 8), grid K * row blocks * class blocks.
 template <typename T, int R>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, R == 8 ? 3 : 4)
 grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_blocks, uint32_t class_blocks) {
   const uint32_t cb = blockIdx.x % class_blocks, kr = blockIdx.x / class_blocks, rb = kr % row_blocks, k = kr / row_blocks;
   const int64_t r0 = ((int64_t)rb * 32 + threadIdx.x) * R;
@@ -742,19 +890,26 @@ grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_block
   if (R > 1 && r0 + R <= v.rows) {
     constexpr int N = vec_n<T>();
     static_assert(R == 1 || R == N, "one vector of rows");
-    uint4 x[8];
+    const int n = c0 < v.classes ? (int)min((int64_t)8, (v.classes - c0 + 7) / 8) : 0;
+    const T* from = src + c0 * v.sc;
+    T* to = dst + c0 * out.sc;
+    const int64_t si = 8 * v.sc, so = 8 * out.sc;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c0 + 8 * e < v.classes) x[e] = *reinterpret_cast<const uint4*>(src + (c0 + 8 * e) * v.sc);
+    for (int h = 0; h < 2; ++h) {  // four vectors in flight at a time
+      uint4 x[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int64_t c = c0 + 8 * e;
-      if (c >= v.classes) break;
-      float l[N];
-      vec_unpack<T>(x[e], l);
+      for (int e = 0; e < 4; ++e)
+        if (4 * h + e < n) x[e] = *reinterpret_cast<const uint4*>(from + (4 * h + e) * si);
 #pragma unroll
-      for (int j = 0; j < N; ++j) l[j] = row[R > 1 ? j : 0](l[j], c);
-      *reinterpret_cast<uint4*>(dst + c * out.sc) = vec_pack<T>(l);
+      for (int e = 0; e < 4; ++e)
+        if (4 * h + e < n) {
+          const int32_t c = (int32_t)c0 + 8 * (4 * h + e);
+          float l[N];
+          vec_unpack<T>(x[e], l);
+#pragma unroll
+          for (int j = 0; j < N; ++j) l[j] = row[R > 1 ? j : 0](l[j], c);
+          *reinterpret_cast<uint4*>(to + (4 * h + e) * so) = vec_pack<T>(l);
+        }
     }
   } else {
     for (int e = 0; e < 8; ++e) {
@@ -762,7 +917,7 @@ grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_block
       if (c >= v.classes) break;
 #pragma unroll
       for (int j = 0; j < R; ++j)
-        if (r0 + j < v.rows) dst[c * out.sc + j] = from_float<T>(row[j](to_float(src[c * v.sc + j]), c));
+        if (r0 + j < v.rows) dst[c * out.sc + j] = from_float<T>(row[j](to_float(src[c * v.sc + j]), (int32_t)c));
     }
   }
 }

@@ -84,25 +84,19 @@ head_score_simt_kernel(const T* __restrict__ h, const T* __restrict__ w, HeadArg
   }
 }
 
-// Joins the partial statistics of a row in a fixed order: 32 rows per block (threadIdx.x), partials y, y + 32, ... per thread, then the 32
-// sums in ascending order of a tree.  grid ceil(total / 32), block (32, 32)
-__global__ void __launch_bounds__(1024)
+// Joins the partial statistics of a row in a fixed order: a warp per row, lane i takes partials i, i + 32, ..., then the lanes meet.
+// grid ceil(total / 8), block 256
+__global__ void __launch_bounds__(256)
 head_join_kernel(HeadArgs a, int64_t total, ScoreOut o) {
   grid_dep_wait();
-  __shared__ float red[3][32][33];
-  const int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  const int lane = threadIdx.x & 31;
+  const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (r >= total) return;
   RowStat st = stat_empty();
-  if (i < total)
-    for (int p = threadIdx.y; p < a.parts; p += 32) st = stat_merge(st, a.part[(int64_t)p * total + i]);
-  red[0][threadIdx.y][threadIdx.x] = st.m;
-  red[1][threadIdx.y][threadIdx.x] = st.s;
-  red[2][threadIdx.y][threadIdx.x] = st.t;
-  __syncthreads();
-  // turned: warp y joins row y of the block over its 32 lanes
-  st = {red[0][threadIdx.x][threadIdx.y], red[1][threadIdx.x][threadIdx.y], red[2][threadIdx.x][threadIdx.y]};
-  for (int d = 16; d > 0; d >>= 1) st = stat_merge(st, stat_shfl_xor(st, d));
-  const int64_t r = (int64_t)blockIdx.x * 32 + threadIdx.y;
-  if (threadIdx.x != 0 || r >= total) return;
+#pragma unroll 4
+  for (int p = lane; p < a.parts; p += 32) st = stat_merge(st, a.part[(int64_t)p * total + r]);
+  st = warp_stat(st);
+  if (lane != 0) return;
   const int32_t y = a.labels ? a.labels[r] : 0;
   float lse = 0.f, ent = 0.f, lp = 0.f;
   if (y >= 0) {

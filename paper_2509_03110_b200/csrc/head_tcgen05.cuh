@@ -33,14 +33,14 @@ constexpr int kHtBlocks = kHtMaxN / 64;  // blocks of 32 classes a draining warp
 // came out 2e-6 short.  So a tile's products are summed in chunks of kHtChunk blocks of 64, each in an accumulator of its own, and the chunks
 // are added in registers.
 constexpr int kHtChunk = 12;
-template <bool PAIR> __host__ __device__ constexpr int ht_stages() { return PAIR ? 6 : 4; }
-template <bool PAIR> __host__ __device__ constexpr int ht_stage_bytes() { return (kHtRows + (PAIR ? kHtMaxN / 2 : kHtMaxN)) * kHtK * 2; }
-template <bool PAIR> __host__ __device__ constexpr int ht_smem_bytes() { return ht_stages<PAIR>() * ht_stage_bytes<PAIR>() + 1024 + 256; }
+constexpr int kHtMaxStages = 12, kHtRing = 216 * 1024;  // bytes of the ring
+constexpr int kHtSmem = kHtRing + 1024 + 512;
 
 struct HeadTile {
   int tile_n, run;     // classes of a tile, consecutive tiles of a unit of work
   int n_tiles, m_tiles, runs;
   int a_rows;          // rows of h a load brings in (a multiple of 8, at most 128)
+  int stages, stage_bytes, a_bytes;  // the ring: [h tile][w tile] per stage, each on a 1024-byte boundary
   int w_shared;        // one head for all workers
   uint32_t idesc;
   int64_t units;       // K * runs * m_tiles
@@ -88,16 +88,16 @@ __device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int6
 template <bool PAIR>
 __global__ void __launch_bounds__(kHtThreads, 1)
 head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_constant__ CUtensorMap map_w, HeadArgs a, HeadTile q) {
-  constexpr int STAGES = ht_stages<PAIR>(), A_BYTES = kHtRows * kHtK * 2;
+  const int STAGES = q.stages, A_BYTES = q.a_bytes, STAGE = q.stage_bytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(ring + STAGES * ht_stage_bytes<PAIR>());
-  uint64_t* empty = full + STAGES;
-  uint64_t* acc_full = empty + STAGES;   // [2]
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + kHtRing);  // [stages]
+  uint64_t* empty = full + kHtMaxStages;
+  uint64_t* acc_full = empty + kHtMaxStages;  // [2]
   uint64_t* acc_empty = acc_full + 2;    // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * STAGES + 4) * 8 + 8 <= 256, "barrier area");
+  static_assert((2 * kHtMaxStages + 4) * 8 + 8 <= 512, "barrier area");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
@@ -138,10 +138,12 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
         const int r0 = (mt * (PAIR ? 2 : 1) + (int)rank) * kHtRows, kw = q.w_shared ? 0 : k;
         const int nt_end = min(q.n_tiles, (rn + 1) * q.run);
         for (int nt = rn * q.run; nt < nt_end && ok; ++nt) {
+          const int k_first = PAIR ? 0 : (int)((int64_t)nt * k_blocks / q.n_tiles);
           const int c0 = nt * q.tile_n + (int)rank * b_rows;
-          for (int kb = 0; kb < k_blocks; ++kb) {
+          for (int kq = 0; kq < k_blocks; ++kq) {
+            const int kb = kq + k_first < k_blocks ? kq + k_first : kq + k_first - k_blocks;
             if (!tc::mbar_wait(&empty[s], ph ^ 1u, abort_flag)) { ok = false; break; }
-            uint8_t* dst = ring + s * ht_stage_bytes<PAIR>();
+            uint8_t* dst = ring + s * STAGE;
             if (PAIR) {
               if (leader) tc::mbar_expect_tx(&full[s], 2 * stage_tx);
               const uint32_t bar = tc::map_to_cta(tc::smem_u32(&full[s]), 0u);
@@ -171,7 +173,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
             const uint32_t d = tmem_base + (uint32_t)as * kHtMaxN;
             if (!tc::mbar_wait(&full[s], ph, abort_flag)) { ok = false; break; }
             tc::tc_fence_after();
-            const uint32_t pa = tc::smem_u32(ring + s * ht_stage_bytes<PAIR>()), pb = pa + A_BYTES;
+            const uint32_t pa = tc::smem_u32(ring + s * STAGE), pb = pa + A_BYTES;
 #pragma unroll
             for (int k = 0; k < kHtK / 16; ++k) {
               const uint64_t ad = tc::smem_desc(pa + k * 32, 16, 1024), bd = tc::smem_desc(pb + k * 32, 16, 1024);
@@ -288,6 +290,12 @@ inline HeadTile ht_plan(int32_t K, int64_t rows, int64_t classes) {
   }
   q.units = (int64_t)K * q.m_tiles * q.runs;
   q.a_rows = pair ? kHtRows : (int)round_up(rows, 8);
+  // few rows: the h tile is as small as they are, and the ring as deep as it can be (the rows of the tile that are not there are whatever lies
+  // behind it in the ring, which leaves the accumulators of the rows that are alone)
+  q.a_bytes = (int)round_up(q.a_rows * kHtK * 2, 1024);
+  q.stage_bytes = q.a_bytes + (pair ? q.tile_n / 2 : q.tile_n) * kHtK * 2;
+  q.stages = std::min(kHtMaxStages, kHtRing / q.stage_bytes);
+  while ((q.stages - 1) * q.stage_bytes + kHtRows * kHtK * 2 > kHtRing) --q.stages;  // 128 rows' worth behind the last stage's start
   return q;
 }
 
@@ -320,7 +328,7 @@ inline bool ht_launch(const T* h, const T* w, HeadArgs a, int32_t K, HeadTile q,
   if (!std::is_same<T, bf16>::value) q.idesc &= ~((1u << 7) | (1u << 10));  // operands f16 instead of bf16
   a.parts = 2 * q.runs;
   const void* kern = pair ? (const void*)head_tcgen05_kernel<true> : (const void*)head_tcgen05_kernel<false>;
-  const int smem = pair ? ht_smem_bytes<true>() : ht_smem_bytes<false>();
+  const int smem = kHtSmem;
   if ((*e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return true;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];

@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <type_traits>
 
 #include "common.cuh"
 #include "dropout.cuh"
@@ -91,8 +92,8 @@ cudaError_t launch_row(const LogitView<T>& v, const int32_t* labels, const Score
   return cudaLaunchKernelEx(&cfg, logprob_row_kernel<T, NT, CS>, v, labels, out);
 }
 
-// Which form a call takes.  Sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 4 KB, 128 threads up
-// to 32 KB, 256 up to 128 KB, 512 beyond; rows of 32 KB and more that leave most of the machine idle are split over a cluster of 8 or 4 blocks
+// Which form a call takes.  Sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 1024 classes, 128 threads
+// up to 32 KB, 256 beyond; rows of 32 KB and more that leave most of the machine idle are split over a cluster of 8 or 4 blocks
 // (4 rows of 131072 bf16, 8 alternatives: 14.4 us with one block a row, 8.3 with eight; 64 rows: 14.4, four blocks 10.7).
 template <typename T>
 cudaError_t launch_scores(const LogitView<T>& v, const int32_t* labels, const ScoreOut& out, int32_t K, cudaStream_t stream) {
@@ -102,13 +103,19 @@ cudaError_t launch_scores(const LogitView<T>& v, const int32_t* labels, const Sc
     logprob_feature_kernel<T><<<(unsigned)(K * row_blocks), feat_rows<T>() * kFeatG, 0, stream>>>(v, labels, out, (uint32_t)row_blocks);
     return cudaPeekAtLastError();
   }
+  if (v.classes <= kWarpClasses) {
+    const int64_t es = sizeof(T);
+    const bool vec = v.sc == 1 && reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && (v.rows == 1 || v.sr * es % 16 == 0) && (K == 1 || v.sk * es % 16 == 0);
+    const unsigned blocks = (unsigned)ceil_div(total, 8);
+    if (vec) logprob_warp_kernel<T, true><<<blocks, 256, 0, stream>>>(v, labels, out, (uint32_t)total);
+    else logprob_warp_kernel<T, false><<<blocks, 256, 0, stream>>>(v, labels, out, (uint32_t)total);
+    return cudaPeekAtLastError();
+  }
   const int64_t bytes = (int64_t)v.classes * sizeof(T);
   if (bytes >= 32768 && total <= 148 / 4) return launch_row<T, 256, 8>(v, labels, out, total, stream);
   if (bytes >= 32768 && total <= 148) return launch_row<T, 256, 4>(v, labels, out, total, stream);
-  if (bytes <= 4096) return launch_row<T, 32, 1>(v, labels, out, total, stream);
   if (bytes <= 32768) return launch_row<T, 128, 1>(v, labels, out, total, stream);
-  if (bytes <= 131072) return launch_row<T, 256, 1>(v, labels, out, total, stream);
-  return launch_row<T, 512, 1>(v, labels, out, total, stream);
+  return launch_row<T, 256, 1>(v, labels, out, total, stream);
 }
 
 }  // namespace
@@ -160,15 +167,19 @@ cudaError_t launch_grad(const LogitView<T>& v, const GradIn& in, const GradOut<T
     }
   }
   const bool vec = v.sc == 1 && o.sc == 1 && (pi - po) % 16 == 0 && (v.rows == 1 || aligned(v.sr - o.sr)) && (K == 1 || aligned(v.sk - o.sk));
-  const bool narrow = v.classes <= 1024;  // a warp per row
+  const bool unit = v.sc == 1 && o.sc == 1, narrow = v.classes <= 1024;  // narrow: a warp per row
   const auto go = [&](auto kern, int64_t chunk) {
     const int64_t chunks = ceil_div(v.classes, chunk), units = total * chunks, blocks = narrow ? ceil_div(units, 8) : units;
     if (units > kMaxIndex) return cudaErrorInvalidConfiguration;
-    kern<<<(unsigned)blocks, 256, 0, stream>>>(v, in, o, (uint32_t)chunks, (uint32_t)units);
+    kern<<<(unsigned)blocks, 256, 0, stream>>>(v, in, o, FastDiv((uint32_t)chunks), (uint32_t)units);
     return cudaPeekAtLastError();
   };
-  if (vec) return narrow ? go(grad_row_kernel<T, 32, true>, grad_chunk<true, T>(32)) : go(grad_row_kernel<T, 256, true>, grad_chunk<true, T>(256));
-  return narrow ? go(grad_row_kernel<T, 32, false>, grad_chunk<false, T>(32)) : go(grad_row_kernel<T, 256, false>, grad_chunk<false, T>(256));
+  const auto pick = [&](auto mode) {
+    constexpr int M = decltype(mode)::value;
+    return narrow ? go(grad_row_kernel<T, 32, M>, grad_chunk<T>(M, 32)) : go(grad_row_kernel<T, 256, M>, grad_chunk<T>(M, 256));
+  };
+  if (vec) return pick(std::integral_constant<int, GRAD_VECTORS>());
+  return unit ? pick(std::integral_constant<int, GRAD_UNIT>()) : pick(std::integral_constant<int, GRAD_ANY>());
 }
 
 }  // namespace
@@ -279,7 +290,7 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)ceil_div(total, 32)); cfg.blockDim = dim3(32, 32); cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)ceil_div(total, 8)); cfg.blockDim = dim3(256); cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = 1;
     e = cudaLaunchKernelEx(&cfg, head_join_kernel, a, total, out);
   }
   return err.done(e);
@@ -304,8 +315,9 @@ cudaError_t launch_dropout(const T* x, const T* skip, T* out, DropArgs a, int32_
     }
   }
   const int64_t segments = ceil_div(a.n, 256), total = segments * a.rows * K;
-  if (ceil_div(total, 8) > kMaxIndex) return cudaErrorInvalidConfiguration;
-  dropout_elem_kernel<T><<<(unsigned)ceil_div(total, 8), 256, 0, stream>>>(x, skip, out, a, segments, total);
+  a.by_groups = FastDiv((uint32_t)segments);
+  a.by_rows = FastDiv((uint32_t)a.rows);
+  dropout_elem_kernel<T><<<(unsigned)ceil_div(total, 8), 256, 0, stream>>>(x, skip, out, a, (uint32_t)total);
   return cudaPeekAtLastError();
 }
 
@@ -326,7 +338,7 @@ extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, in
       (d_skip && !strides_ok(K, skip_stride_k, rows, skip_stride_row, n, 1)))
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
   if ((K > 1 && out_stride_k == 0) || (rows > 1 && out_stride_row < n)) return err.fail(LSAM_ERR_INVALID, "elements of the output share an address");
-  if ((__int128)ceil_div(n, 8) * rows * K >= ((__int128)1 << 38)) return err.fail(LSAM_ERR_INVALID, "K * rows * ceil(n / 8) must be below 2^38");
+  if ((__int128)ceil_div(n, 256) * rows * K > kMaxIndex) return err.fail(LSAM_ERR_INVALID, "K * rows * ceil(n / 256) must be below 2^31");
   PtrCheck pc;
   pc.need(d_x, dtype_size(dtype)); pc.need(d_out, dtype_size(dtype)); pc.optional(d_skip, dtype_size(dtype));
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);

@@ -60,7 +60,7 @@ def test_head_refuses(kw, code, word):
 @pytest.mark.parametrize("kw, word", [
     (dict(dtype=3), "dtype"), (dict(p=-0.1), "p outside"), (dict(p=1.01), "p outside"), (dict(p=float("nan")), "p outside"), (dict(n=-1), "negative"), (dict(layer=-1), "layer"), (dict(layer=4096), "layer"),
     (dict(k_offset=-1), "workers"), (dict(k_offset=(1 << 20) - 1, K=2), "workers"), (dict(n=1 << 31), "2^31"), (dict(xr=-1), "stride"), (dict(orow=4), "address"), (dict(K=2, ok=0), "address"),
-    (dict(rows=(1 << 31) - 1, n=(1 << 31) - 1, orow=(1 << 31) - 1, xr=0), "stride|2^38")])
+    (dict(rows=(1 << 31) - 1, n=(1 << 31) - 1, orow=(1 << 31) - 1, xr=0), "stride|2^31")])
 def test_dropout_refuses(kw, word):
     rc, msg = _dropout(**kw)
     assert rc == G.LSAM_ERR_INVALID and any(w in msg for w in word.split("|")), (rc, msg)
