@@ -188,20 +188,32 @@ def _invalid(msg):
     return LsamError(LSAM_ERR_INVALID, msg)
 
 
-_torch = None
+# Host time is what bounds the smallest calls (an allocation through torch.empty with keywords is 2 to 3 us, a stream object 2 us), so the
+# operators allocate through an empty tensor of the right type and device, and ask for the stream's handle alone.
+_torch = _raw_stream = None
 _codes = {}  # torch dtype -> LSAM_FP32 / LSAM_BF16 / LSAM_FP16
+_protos = {}  # device -> (empty float32 tensor, empty int32 tensor): what results are allocated like; they hold no memory
 _err = threading.local()  # one message buffer per thread
 
 
 def _load():
     """torch, imported with the first operator call."""
-    global _torch
+    global _torch, _raw_stream
     if _torch is None:
         import torch
 
         _codes.update({torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16})
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _raw_stream = (lambda dev: raw(dev.index)) if raw is not None else (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
         _torch = torch
     return _torch
+
+
+def _proto(dev):
+    p = _protos.get(dev)
+    if p is None:
+        p = _protos[dev] = tuple(_torch.empty(0, dtype=t, device=dev) for t in (_torch.float32, _torch.int32))
+    return p
 
 
 def _call(fn, *args):
@@ -237,7 +249,7 @@ def _ptr(t, what, shape, dtype, dev):
     """Address of a dense per-row array, None if it is not given."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != dev:
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise _invalid(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
     return t.data_ptr()
 
@@ -263,18 +275,19 @@ def lsam_logprob(logits, labels=None, top_k=0, stream=None):
     dev = logits.device
     lead = logits.shape[:-1]
     pl = None if labels is None else _ptr(labels, "labels", lead, torch.int32, dev)
-    logp = None if labels is None else torch.empty(lead, dtype=torch.float32, device=dev)
-    lse = torch.empty(lead, dtype=torch.float32, device=dev)
-    ent = torch.empty(lead, dtype=torch.float32, device=dev)
+    f32, i32 = _proto(dev)
+    lse = f32.new_empty(lead)
+    ent = torch.empty_like(lse)
+    logp = None if labels is None else torch.empty_like(lse)
     tv = ti = pv = pi = None
     if top_k:
         if not 0 < top_k <= TOP_MAX:
             raise _invalid(f"top_k outside 0 .. {TOP_MAX}")
-        tv = torch.empty((*lead, top_k), dtype=torch.float32, device=dev)
-        ti = torch.empty((*lead, top_k), dtype=torch.int32, device=dev)
+        shape = (*lead, top_k)
+        tv, ti = f32.new_empty(shape), i32.new_empty(shape)
         pv, pi = tv.data_ptr(), ti.data_ptr()
     _call(lib().lsam_logprob, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, top_k, None if logp is None else logp.data_ptr(), lse.data_ptr(), ent.data_ptr(), pv, pi,
-          torch.cuda.current_stream(dev).cuda_stream)
+          _raw_stream(dev))
     return LogProb(logp, lse, ent, tv, ti)
 
 
@@ -302,7 +315,7 @@ def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, o
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
         raise _invalid("out must have the shape, type and device of logits")
     ok, orow, oc = _stacked(out, "out")[3:]
-    _call(lib().lsam_logprob_grad, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, ps, pe, pa, pb, out.data_ptr(), ok, orow, oc, torch.cuda.current_stream(dev).cuda_stream)
+    _call(lib().lsam_logprob_grad, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, ps, pe, pa, pb, out.data_ptr(), ok, orow, oc, _raw_stream(dev))
     return out
 
 
@@ -329,14 +342,15 @@ def lsam_head_logprob(h, w, labels=None, bias=None, stream=None):
     if bias is not None:
         pb = _ptr(bias, "bias", (V,) if bias.dim() == 1 else (K, V), torch.float32, dev)
         bk = V if bias.dim() == 2 else 0
-    logp = None if labels is None else torch.empty(lead, dtype=torch.float32, device=dev)
-    lse = torch.empty(lead, dtype=torch.float32, device=dev)
-    ent = torch.empty(lead, dtype=torch.float32, device=dev)
+    f32 = _proto(dev)[0]
+    lse = f32.new_empty(lead)
+    ent = torch.empty_like(lse)
+    logp = None if labels is None else torch.empty_like(lse)
     L = lib()
     nbytes = L.lsam_head_logprob_workspace_bytes(K, R, V)
-    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
+    ws = f32.new_empty(nbytes // 4 + 64)
     _call(L.lsam_head_logprob, h.data_ptr(), w.data_ptr(), pb, code, K, R, D, V, hk, hr, wk, wc, bk, pl, None if logp is None else logp.data_ptr(), lse.data_ptr(),
-          ent.data_ptr(), (ws.data_ptr() + 255) // 256 * 256, nbytes, torch.cuda.current_stream(dev).cuda_stream)
+          ent.data_ptr(), (ws.data_ptr() + 255) // 256 * 256, nbytes, _raw_stream(dev))
     return LogProb(logp, lse, ent, None, None)
 
 
@@ -355,7 +369,7 @@ def lsam_dropout(x, p, seed, tick, layer=0, k_offset=0, skip=None, out=None, str
     if not 0 <= seed < 1 << 64 or not 0 <= tick < 1 << 64:
         raise _invalid("seed and tick are unsigned 64-bit numbers")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        out = x.new_empty(x.shape)
     elif out.shape != x.shape or out.dtype != x.dtype or out.device != dev:
         raise _invalid("out must have the shape, type and device of x")
     ok, orow, oc = _stacked(out, "out")[3:]
@@ -368,7 +382,7 @@ def lsam_dropout(x, p, seed, tick, layer=0, k_offset=0, skip=None, out=None, str
     if (xc != 1 or oc != 1 or sc != 1) and n > 1:
         raise _invalid("the columns of x, skip and out must be contiguous")
     _call(lib().lsam_dropout, x.data_ptr(), ps, out.data_ptr(), code, K, R, n, xk, xr, sk, sr, ok, orow, p, seed, tick, layer, k_offset,
-          torch.cuda.current_stream(dev).cuda_stream)
+          _raw_stream(dev))
     return out
 
 

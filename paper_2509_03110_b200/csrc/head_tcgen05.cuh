@@ -272,6 +272,10 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
 // tiles; a tile costs its width plus the share of h it takes in (measured as 32 classes' worth).  Longer runs leave fewer partial statistics.
 // 32768 classes, 4 rows: 147 tiles of 224 instead of 128 of 256, so that every SM streams its share of w.
 inline HeadTile ht_plan(int32_t K, int64_t rows, int64_t classes) {
+  // the search takes a few microseconds: the last one of a thread is kept, by its sizes
+  struct Last { int32_t K = 0; int64_t rows = 0, classes = 0; HeadTile q{}; };
+  static thread_local Last last;
+  if (last.K == K && last.rows == rows && last.classes == classes) return last.q;
   HeadTile q{};
   const bool pair = rows > kHtRows;
   const int64_t ctas = pair ? 74 : 148;
@@ -296,6 +300,7 @@ inline HeadTile ht_plan(int32_t K, int64_t rows, int64_t classes) {
   q.stage_bytes = q.a_bytes + (pair ? q.tile_n / 2 : q.tile_n) * kHtK * 2;
   q.stages = std::min(kHtMaxStages, kHtRing / q.stage_bytes);
   while ((q.stages - 1) * q.stage_bytes + kHtRows * kHtK * 2 > kHtRing) --q.stages;  // 128 rows' worth behind the last stage's start
+  last = {K, rows, classes, q};
   return q;
 }
 
