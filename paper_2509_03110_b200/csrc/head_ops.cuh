@@ -18,12 +18,12 @@ __device__ inline float ex2(float x) {
   return y;
 }
 
-// Running statistics of a set of logits, held relative to its maximum m (NaN ignored) in units of log 2.  With k = kLog2e, B = fl(m k)
-// and w = l k - B (one fused multiply-add):  s = sum 2^w,  t = sum 2^w w,  so that
-//   logsumexp = m + (log2 s - (m k - B)) / k,   entropy = -sum p log p = (log2 s - t / s) / k.
-// B is the reference itself, not an approximation of m k, and k's own rounding only scales the logits by 1 + 1e-8: an offset common to all
-// logits costs no digits of the entropy or of a log probability.  Logits at or below kMasked are masks: they enter as kMasked, whose 2^w is 0
-// beside any other (and (-inf) * 0 never arises); a set of nothing but masks has m = kMasked.  A NaN or +inf logit makes s NaN.
+// Running statistics of a set of logits, held relative to its maximum m (NaN ignored) in units of log 2.  With k = kLog2e and w = (l - m) k:
+//   s = sum 2^w,  t = sum 2^w w,  logsumexp = m + log2 s / k,   entropy = -sum p log p = (log2 s - t / s) / k.
+// The difference l - m comes first: near the maximum it is exact, so an offset common to all logits, however large, costs no digits of the entropy
+// or of a log probability (l k - m k in one multiply-add would be off by the rounding of m k: 2^85 at m = -1e9, a usual mask).
+// Logits at or below kMasked are masks: they enter as kMasked, whose 2^w is 0 beside any other (and (-inf) * 0 never arises); a set of nothing but
+// masks has m = kMasked.  A NaN or +inf logit makes s NaN.
 constexpr float kMasked = -1e30f;
 __device__ inline float above_masked() { return __uint_as_float(__float_as_uint(kMasked) - 1u); }  // the least fp32 number above it
 struct RowStat { float m, s, t; };
@@ -34,7 +34,7 @@ __device__ inline float max_nan(float a, float b) {  // NaN if either is
 }
 __device__ inline RowStat stat_empty() { return {kMasked, 0.f, 0.f}; }
 __device__ inline void stat_rebase(RowStat& a, float m) {  // express a's sums relative to m >= a.m
-  const float d = __fmul_rn(a.m, kLog2e) - __fmul_rn(m, kLog2e);  // the difference of the two references: never contracted
+  const float d = fmaxf((a.m - m) * kLog2e, -1000.f);  // 2^-1000 is 0, and d s stays finite
   const float f = ex2(d);
   a.t = f * fmaf(d, a.s, a.t);
   a.s *= f;
@@ -43,7 +43,7 @@ __device__ inline void stat_rebase(RowStat& a, float m) {  // express a's sums r
 __device__ inline void stat_add(RowStat& a, float l) {  // one logit, masks and NaN included
   l = max_nan(l, kMasked);
   if (l > a.m) stat_rebase(a, l);
-  const float w = fmaf(l, kLog2e, -(a.m * kLog2e));
+  const float w = (l - a.m) * kLog2e;
   const float e = ex2(w);
   a.s += e;
   a.t = fmaf(e, w, a.t);
@@ -72,13 +72,13 @@ __device__ inline RowStat warp_stat(RowStat a) {
   }
   return a;
 }
-struct RowScore { float B, ls, lse, ent; };
+struct RowScore { float m, ls, lse, ent; };  // ls = lse - m
 __device__ inline RowScore stat_finish(const RowStat& a) {
   if (a.m <= kMasked && a.s == a.s) return {0.f, 0.f, -INFINITY, 0.f};
-  const float B = a.m * kLog2e, ls = log2f(a.s);
-  return {B, ls, a.m + (ls - fmaf(a.m, kLog2e, -B)) / kLog2e, (ls - a.t / a.s) / kLog2e};
+  const float b = log2f(a.s), ls = b / kLog2e;
+  return {a.m, ls, a.m + ls, (b - a.t / a.s) / kLog2e};
 }
-__device__ inline float score_logp(float l, const RowScore& r) { return l <= kMasked ? -INFINITY : (fmaf(l, kLog2e, -r.B) - r.ls) / kLog2e; }
+__device__ inline float score_logp(float l, const RowScore& r) { return l <= kMasked ? -INFINITY : (l - r.m) - r.ls; }
 
 // Order of the alternatives: larger logit first, then the lower class.  One 64-bit key per element (0: not an alternative,
 // i.e. a mask or NaN); -0 and +0 are one value.
@@ -149,6 +149,11 @@ __device__ inline uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+__device__ inline uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ inline uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -159,12 +164,11 @@ template <int N>
 __device__ inline void stat_add_all(RowStat& a, const float (&l)[N], float mx) {
   static_assert(N % 2 == 0, "pairs");
   if (mx > a.m) stat_rebase(a, mx);
-  const float nb = -__fmul_rn(a.m, kLog2e);
-  const uint64_t k2 = pack2(kLog2e, kLog2e), nb2 = pack2(nb, nb);
+  const uint64_t k2 = pack2(kLog2e, kLog2e), m2 = pack2(-a.m, -a.m);
   uint64_t s2 = 0, t2 = 0;
 #pragma unroll
   for (int j = 0; j < N; j += 2) {
-    const uint64_t w2 = fma2(pack2(l[j], l[j + 1]), k2, nb2);
+    const uint64_t w2 = mul2(add2(pack2(l[j], l[j + 1]), m2), k2);
     float w0, w1;
     unpack2(w2, w0, w1);
     const uint64_t e2 = pack2(ex2(w0), ex2(w1));

@@ -71,17 +71,7 @@ __device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int6
     l[j] = max_nan(l[j], kMasked);
     mx = fmaxf(mx, l[j]);
   }
-  if (mx > st.m) stat_rebase(st, mx);
-  const float B = __fmul_rn(st.m, kLog2e);
-  float s2[2] = {0.f, 0.f}, t2[2] = {0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    const float w = fmaf(l[j], kLog2e, -B), e = ex2(w);
-    s2[j & 1] += e;
-    t2[j & 1] = fmaf(e, w, t2[j & 1]);
-  }
-  st.s += s2[0] + s2[1];
-  st.t += t2[0] + t2[1];
+  stat_add_all(st, l, mx);
 }
 
 // grid: CTAs (pairs: clusters of 2), each walking units u, u + grid, ...; unit = (run of class tiles, row tile) of a worker, row tile fastest

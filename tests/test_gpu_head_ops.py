@@ -81,7 +81,7 @@ def close(got, want, tol):
     tol = np.broadcast_to(tol.cpu().numpy() if isinstance(tol, torch.Tensor) else tol, want.shape)
     fine = np.isfinite(want)
     np.testing.assert_array_equal(got[~fine], want[~fine])
-    bad = np.abs(got[fine] - want[fine]) > tol[fine]
+    bad = ~(np.abs(got[fine] - want[fine]) <= tol[fine])  # a NaN is never within
     assert not bad.any(), (got[fine][bad][:5], want[fine][bad][:5], tol[fine][bad][:5])
 
 
@@ -123,7 +123,7 @@ def test_scores(size, layout, dtype):
 @pytest.mark.parametrize("layout", ["row", "feature"])
 @pytest.mark.parametrize("C", [10, 257, 1000, 4100, 40001])
 def test_scores_of_masked_rows(C, layout):
-    rows = 12
+    rows = 16
     l = make_logits(1, rows, C, "fp32", layout, seed=3)
     l[0, 0] = NINF                       # nothing left
     l[0, 1] = NINF; l[0, 1, C // 2] = 1.5  # one class left
@@ -137,6 +137,10 @@ def test_scores_of_masked_rows(C, layout):
     l[0, 9] = 0.0                        # every class equal
     l[0, 10] = -0.0; l[0, 10, 1] = 0.0
     l[0, 11, :] = NINF; l[0, 11, 3] = NAN
+    l[0, 12, 1:] = -1e9                  # usual masks, and whole rows of large numbers
+    l[0, 13] = -1e10
+    l[0, 14] = 2e38; l[0, 14, 0] = 1e38  # the documented end of the range
+    l[0, 15] = NINF; l[0, 15, C - 2:] = 0.5  # a few classes at the end
     y = torch.full((1, rows), 1, device="cuda", dtype=torch.int32)
     for k in (1, 8, 32):
         check_scores(l, y, k)
@@ -193,6 +197,7 @@ def grad_reference(l, y, lse, ent, a, b):
     none = torch.isneginf(lse)  # nothing but masks
     none = none if y is None else none | (y < 0)
     g = torch.where(none.unsqueeze(-1), torch.zeros_like(g), g)
+    err = torch.where(none.unsqueeze(-1), torch.zeros_like(err), err)  # exactly zero there, whatever the logits hold
     if y is not None:
         g = torch.where((y >= l.shape[-1]).unsqueeze(-1), torch.full_like(g, NAN), g)
     fi = torch.finfo(l.dtype)
