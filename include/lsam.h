@@ -39,6 +39,8 @@ extern "C" {
 
 typedef struct lsam_ctx lsam_ctx;
 
+#define LSAM_TOP_MAX 32 /* most alternatives a scoring call returns */
+
 enum {
   LSAM_OK = 0,
   LSAM_ERR_INVALID = 1,   /* bad argument or configuration                                          */
@@ -190,6 +192,16 @@ int lsam_step_batch(lsam_ctx* ctx, float eta, float rho, const float* xb, const 
 int lsam_stage_batch(lsam_ctx* ctx, const float* xb, const void* yb, int on_host);
 int lsam_step_staged(lsam_ctx* ctx, float eta, float rho, float* h_loss);
 
+/* Scores of a minibatch under the workers' iterates x_k, without training on them (classifiers only): the forward pass of every worker on its
+ * rows of xb, then lsam_logprob (end of this header, whose rules for labels, masks and ties hold) on the logits.
+ *  xb [K, B, widths[0]] fp32, yb [K, B] int32 labels or NULL; both on the host (on_host = 1) or on the device (0).
+ *  d_logp (needs yb), d_lse, d_entropy [K, B] and d_top_logp, d_top_idx [K, B, top_k]: device memory, nullable (top_k = 0: no alternatives).
+ * No state of the run changes: a tick after this call is bit for bit the tick without it.  Every worker is scored, also one that waits (active_num).
+ * The centre is scored by a context that was given it as x0.  Asynchronous on the context's stream: pinned host arrays must stay as they are until
+ * the stream has passed the call.  LSAM_ERR_STATE while a minibatch is staged. */
+int lsam_score_batch(lsam_ctx* ctx, const float* xb, const int32_t* yb, int on_host, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
+                     float* d_top_logp, int32_t* d_top_idx);
+
 /* Sync branch of Algorithm 2 (centre update with look-ahead, counters reset).  Returns LSAM_ERR_STATE and does
  * nothing when the trigger (sum_k t_x[k] > 0 and sum_k t_x[k] mod K tau == 0) is false. */
 int lsam_couple(lsam_ctx* ctx);
@@ -331,8 +343,7 @@ enum { LSAM_FP32 = 0, LSAM_BF16 = 1, LSAM_FP16 = 2 };
  *  d_logp (needs d_labels), d_lse, d_entropy: nullable.  top_k = 0 .. LSAM_TOP_MAX; with 0 the two top arrays are not touched.
  * Logits at or below -1e30 are masks (-inf, or the lowest value of bf16 and fp32): probability 0, log probability -inf, never alternatives.
  * Missing alternatives have index -1 and log probability -inf; a row of nothing but masks has lse = -inf, logp = -inf, entropy 0.  A NaN or a
- * +inf logit (from 2e38 on) makes lse, entropy and every log probability of its row NaN (a masked label keeps -inf); NaN is never an alternative. */
-#define LSAM_TOP_MAX 32
+ * +inf logit (or one above 2e38, where differences of logits leave the fp32 range) makes lse, entropy and every log probability of its row NaN (a masked label keeps -inf); NaN is never an alternative. */
 int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                  int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
                  float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len);

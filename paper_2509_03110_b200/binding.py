@@ -29,7 +29,7 @@ EXPORTS = [
     "lsam_profile_enable", "lsam_profile_read", "lsam_launch_count", "lsam_uses_tcgen05", "lsam_last_error",
     "lsam_destroy", "lsam_schedule_hash", "lsam_row_norms_static", "lsam_acc_buffer", "lsam_selftest_bounded_wait",
     "lsam_checkpoint_bytes", "lsam_save_checkpoint", "lsam_load_checkpoint", "lsam_read_anchor_gap",
-    "lsam_logprob", "lsam_logprob_grad", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout",
+    "lsam_logprob", "lsam_logprob_grad", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout", "lsam_score_batch",
 ]
 
 
@@ -77,6 +77,7 @@ def lib():
     L.lsam_step_batch.argtypes = [vp, C.c_float, C.c_float, vp, vp, C.c_int, vp]
     L.lsam_stage_batch.argtypes = [vp, vp, vp, C.c_int]
     L.lsam_step_staged.argtypes = [vp, C.c_float, C.c_float, vp]
+    L.lsam_score_batch.argtypes = [vp, vp, vp, C.c_int, C.c_int32, vp, vp, vp, vp, vp]
     L.lsam_couple.argtypes = [vp]
     L.lsam_acc_buffer.argtypes = [vp, C.POINTER(vp), C.POINTER(C.c_int64)]
     L.lsam_should_couple.argtypes = [vp]
@@ -464,6 +465,35 @@ class Lsam:
 
     def step_staged(self, eta, rho, h_loss=None):
         self._check(lib().lsam_step_staged(self._h, eta, rho, _np_ptr(h_loss)))
+
+    def score_batch(self, xb, yb=None, top_k=0):
+        """Log probability of the labels, log-sum-exp, entropy and top_k alternatives of a minibatch under every worker's iterate.
+
+        xb [K, B, in] float32, yb [K, B] int32 or None: both CUDA tensors, or both host tensors / numpy arrays.  Returns LogProb of CUDA tensors [K, B].
+        """
+        torch = _load()
+        if not 0 <= top_k <= TOP_MAX:
+            raise _invalid(f"top_k outside 0 .. {TOP_MAX}")
+        K, B = self.K, self.cfg.batch
+        on_host = not (isinstance(xb, torch.Tensor) and xb.is_cuda)
+        for t, what, ty, shape in ((xb, "xb", "float32", None), (yb, "yb", "int32", (K, B))):
+            if t is None:
+                continue
+            ok = str(t.dtype).replace("torch.", "") == ty and (t.is_contiguous() if isinstance(t, torch.Tensor) else t.flags.c_contiguous)
+            if not ok or tuple(t.shape[:2]) != (K, B) or (shape and tuple(t.shape) != shape) or on_host == (isinstance(t, torch.Tensor) and t.is_cuda):
+                raise _invalid(f"{what} must be a contiguous {ty} array [K, B, ...] on the {'host' if on_host else 'device'}")
+        n_in = self.cfg.widths[0] * (self.cfg.img_h * self.cfg.img_w if self.cfg.model == MODEL_CNN else 1)
+        if int(np.prod(tuple(xb.shape[2:]))) != n_in:
+            raise _invalid(f"a row of xb must hold {n_in} features")
+        with torch.cuda.stream(self.stream):
+            f32, i32 = _proto(self.workspace.device)
+            lse = f32.new_empty((K, B))
+            ent = torch.empty_like(lse)
+            logp = None if yb is None else torch.empty_like(lse)
+            tv, ti = (f32.new_empty((K, B, top_k)), i32.new_empty((K, B, top_k))) if top_k else (None, None)
+        ptr = lambda a: None if a is None else C.c_void_p(a.data_ptr()) if isinstance(a, torch.Tensor) else _np_ptr(a)  # noqa: E731
+        self._check(lib().lsam_score_batch(self._h, ptr(xb), ptr(yb), 1 if on_host else 0, top_k, ptr(logp), ptr(lse), ptr(ent), ptr(tv), ptr(ti)))
+        return LogProb(logp, lse, ent, tv, ti)
 
     def should_couple(self):
         return bool(lib().lsam_should_couple(self._h))

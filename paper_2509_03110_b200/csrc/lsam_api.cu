@@ -616,25 +616,21 @@ int launch_simt(lsam_ctx* c, int cls, GemmOperand A, GemmOperand B, int M, int N
   return LSAM_OK;
 }
 
-// One gradient pass of the classifier at the parameters P ([K, ld], type T); gradient -> g, loss -> loss_out (nullable).
-// g_bf16 (tensor-core path only): store the gradient rounded to bf16 in the g1b buffer instead of fp32 in g.
-// fu != nullptr (tensor-core path, descent pass): the weight gradient of every layer is consumed by the worker update in its own
-// epilogue instead of being stored; the dgrad of a layer, which still reads the perturbed weights, then runs BEFORE that layer's wgrad.
+// A head of at most kHeadMaxOut classes: chunked forward + sum in the loss kernel (SIMT paths, the convolutional model and the three-plane form; the
+// bf16 tensor-core path keeps its GEMM)
+bool narrow_head(const lsam_ctx* c) { return c->L.layers.back().out <= kHeadMaxOut && (!c->use_tc || c->L.x3); }
+
+// Forward of the classifier at the parameters P ([K, ld], type T): activations, ReLU masks and the logits (a narrow head: its partial sums).
 template <typename T>
-int mlp_pass(lsam_ctx* c, const T* P, float* loss_out, bool g_bf16, const TcFusedUpdate* fu = nullptr) {
+int mlp_forward(lsam_ctx* c, const T* P) {
   const Layout& L = c->L;
   const int K = c->cfg.K, B = c->cfg.batch;
   const int nl = (int)L.layers.size();
   const int64_t ld = L.ld;
   const int ldb = L.ldb;
   int rc;
-  // a head of at most kHeadMaxOut classes: chunked forward + sum in the loss kernel (SIMT paths and the three-plane form; the
-  // bf16 tensor-core path keeps its GEMM)
-  const bool narrow = L.layers[nl - 1].out <= kHeadMaxOut && (!c->use_tc || L.x3);
+  const bool narrow = narrow_head(c);
   const int64_t p_plane = L.x3 ? (int64_t)K * ld : 0;
-  // on the SIMT paths the same heads go backward through head_dgrad_kernel (the three-plane form keeps its GEMM, which measured the same)
-  const bool head_bwd = narrow && nl >= 2 && !c->use_tc;
-  // forward
   for (int l = 0; l < nl; ++l) {
     const LayerInfo& li = L.layers[l];
     const T* a_in = c->at<T>(L.act[l]);
@@ -662,6 +658,26 @@ int mlp_pass(lsam_ctx* c, const T* P, float* loss_out, bool g_bf16, const TcFuse
     }
     if (rc != LSAM_OK) return rc;
   }
+  return LSAM_OK;
+}
+
+// One gradient pass of the classifier at the parameters P ([K, ld], type T); gradient -> g, loss -> loss_out (nullable).
+// g_bf16 (tensor-core path only): store the gradient rounded to bf16 in the g1b buffer instead of fp32 in g.
+// fu != nullptr (tensor-core path, descent pass): the weight gradient of every layer is consumed by the worker update in its own
+// epilogue instead of being stored; the dgrad of a layer, which still reads the perturbed weights, then runs BEFORE that layer's wgrad.
+template <typename T>
+int mlp_pass(lsam_ctx* c, const T* P, float* loss_out, bool g_bf16, const TcFusedUpdate* fu = nullptr) {
+  const Layout& L = c->L;
+  const int K = c->cfg.K, B = c->cfg.batch;
+  const int nl = (int)L.layers.size();
+  const int64_t ld = L.ld;
+  const int ldb = L.ldb;
+  int rc;
+  const bool narrow = narrow_head(c);
+  const int64_t p_plane = L.x3 ? (int64_t)K * ld : 0;
+  // on the SIMT paths the same heads go backward through head_dgrad_kernel (the three-plane form keeps its GEMM, which measured the same)
+  const bool head_bwd = narrow && nl >= 2 && !c->use_tc;
+  if ((rc = mlp_forward(c, P)) != LSAM_OK) return rc;
   // loss and its gradient w.r.t. the logits
   const int C = L.layers[nl - 1].out;
   int cur = 0;
@@ -743,18 +759,16 @@ int mlp_pass(lsam_ctx* c, const T* P, float* loss_out, bool g_bf16, const TcFuse
   return LSAM_OK;
 }
 
-// One gradient pass of the convolutional model (SIMT GEMMs): convolution layers through an explicit patch matrix, then the
-// dense layers exactly as in mlp_pass.  Feature maps are [K, C, (y, x, sample)] with the sample fastest (see im2col_kernel).
+// Forward of the convolutional model, as mlp_forward.
 template <typename T>
-int cnn_pass(lsam_ctx* c, const T* P, float* loss_out) {
+int cnn_forward(lsam_ctx* c, const T* P) {
   const Layout& L = c->L;
   const int K = c->cfg.K, B = c->cfg.batch;
-  const int nl = (int)L.layers.size(), nconv = c->cfg.n_conv;
+  const int nl = (int)L.layers.size();
   const int64_t ld = L.ld;
   const int ldb = L.ldb;  // = B for this model
-  const bool narrow = L.layers[nl - 1].out <= kHeadMaxOut;  // chunked head forward, summed by the loss kernel
+  const bool narrow = narrow_head(c);
   int rc;
-  // forward
   for (int l = 0; l < nl; ++l) {
     const LayerInfo& li = L.layers[l];
     const T* a_in = c->at<T>(L.act[l]);
@@ -796,6 +810,21 @@ int cnn_pass(lsam_ctx* c, const T* P, float* loss_out) {
     }
     if (rc != LSAM_OK) return rc;
   }
+  return LSAM_OK;
+}
+
+// One gradient pass of the convolutional model (SIMT GEMMs): convolution layers through an explicit patch matrix, then the
+// dense layers exactly as in mlp_pass.  Feature maps are [K, C, (y, x, sample)] with the sample fastest (see im2col_kernel).
+template <typename T>
+int cnn_pass(lsam_ctx* c, const T* P, float* loss_out) {
+  const Layout& L = c->L;
+  const int K = c->cfg.K, B = c->cfg.batch;
+  const int nl = (int)L.layers.size(), nconv = c->cfg.n_conv;
+  const int64_t ld = L.ld;
+  const int ldb = L.ldb;  // = B for this model
+  const bool narrow = narrow_head(c);
+  int rc;
+  if ((rc = cnn_forward(c, P)) != LSAM_OK) return rc;
   const int C = L.layers[nl - 1].out;
   int cur = 0;
   LAUNCH(c, LSAM_PROF_LOSS, launch_k(c, softmax_ce_kernel<T>, dim3((unsigned)ceil_div(B, 32), K), dim3(32, 8), 0, 
@@ -877,6 +906,27 @@ int grad_pass(lsam_ctx* c, bool perturbed, float* loss_out, bool g_bf16 = false,
   if (cfg.gemm_dtype == LSAM_GEMM_BF16) return mlp_pass<bf16>(c, c->at<bf16>(c->L.xop), loss_out, g_bf16 && c->use_tc, c->use_tc ? fu : nullptr);
   if (c->L.x3) return mlp_pass<bf16>(c, c->at<bf16>(c->L.xpl), loss_out, false);  // the planes hold x or x~, whichever was split last
   return mlp_pass<float>(c, perturbed ? c->at<float>(c->L.xop) : c->x(), loss_out, false);
+}
+
+// Logits of the minibatch in act[0] at the workers' iterates -> L.logits [K, C, ldb].
+template <typename T>
+int narrow_logits(lsam_ctx* c, const T* P) {
+  const Layout& L = c->L;
+  const LayerInfo& li = L.layers.back();
+  const int K = c->cfg.K, B = c->cfg.batch;
+  LAUNCH(c, LSAM_PROF_LOSS, launch_k(c, narrow_logits_kernel<T>, dim3((unsigned)ceil_div(B, 128), li.out, K), 128, 0, c->at<float>(L.hpart), (int)ceil_div(li.in, kHeadChunkIn),
+                                     P + li.b_pad, L.ld, L.x3 ? (int64_t)K * L.ld : 0, B, li.out, L.ldb, c->at<float>(L.logits)));
+  return LSAM_OK;
+}
+int forward_pass(lsam_ctx* c) {
+  const auto at = [&](auto* P) -> int {
+    int rc = c->cfg.model == LSAM_MODEL_CNN ? cnn_forward(c, P) : mlp_forward(c, P);
+    if (rc == LSAM_OK && narrow_head(c)) rc = narrow_logits(c, P);
+    return rc;
+  };
+  if (c->cfg.gemm_dtype == LSAM_GEMM_BF16) return at(c->at<bf16>(c->L.xop));  // the operand copy of x
+  if (c->L.x3) return at(c->at<bf16>(c->L.xpl));                              // its three planes
+  return at(c->x());
 }
 
 // x3 form: the three bf16 planes of src [K, ld] (x, or the perturbed point) -> xpl
@@ -1268,6 +1318,50 @@ int lsam_step_batch(lsam_ctx* c, float eta, float rho, const float* xb, const vo
     LSAM_CUDA(c, cudaStreamSynchronize(c->stream));
   }
   return LSAM_OK;
+}
+
+int lsam_score_batch(lsam_ctx* c, const float* xb, const int32_t* yb, int on_host, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
+                     float* d_top_logp, int32_t* d_top_idx) {
+  if (!c || !xb) return LSAM_ERR_INVALID;
+  const lsam_config& cfg = c->cfg;
+  const Layout& L = c->L;
+  if (cfg.model == LSAM_MODEL_FLAT || cfg.model == LSAM_MODEL_LSQ) return c->fail(LSAM_ERR_INVALID, "lsam_score_batch: classifiers only");
+  if (d_logp && !yb) return c->fail(LSAM_ERR_INVALID, "lsam_score_batch: d_logp without labels");
+  if (top_k < 0 || top_k > LSAM_TOP_MAX || (top_k > 0 && (!d_top_logp || !d_top_idx))) return c->fail(LSAM_ERR_INVALID, "lsam_score_batch: top_k outside 0 .. LSAM_TOP_MAX, or its arrays missing");
+  if (c->stage_count > 0) return c->fail(LSAM_ERR_STATE, "lsam_score_batch: a staged minibatch is waiting in the buffers this call would use");
+  if (int rc = c->check_device()) return rc;
+  const int K = cfg.K, B = cfg.batch;
+  const int64_t rows = (int64_t)K * B;
+  const cudaMemcpyKind kind = on_host ? cudaMemcpyHostToDevice : cudaMemcpyDeviceToDevice;
+  float* xdst = c->at<float>(L.xstage);
+  c->launches += 1;
+  LSAM_CUDA(c, cudaMemcpyAsync(xdst, xb, sizeof(float) * rows * L.in0, kind, c->stream));
+  if (yb) {
+    c->launches += 1;
+    LSAM_CUDA(c, cudaMemcpyAsync(c->at<int32_t>(L.ylab), yb, 4 * rows, kind, c->stream));
+  }
+  // unequal progress: every worker is scored, also those that waited at the last tick, whose mask is put back afterwards
+  int32_t* kept = c->sched_scratch() + 3 * K;
+  if (c->async_on) {
+    LSAM_CUDA(c, cudaMemcpyAsync(kept, c->active_buf(), 4 * (size_t)K, cudaMemcpyDeviceToDevice, c->stream));
+    LSAM_CUDA(c, cudaMemsetAsync(c->active_buf(), 1, 4 * (size_t)K, c->stream));
+  }
+  dim3 grid((unsigned)ceil_div(L.in0, 32), (unsigned)ceil_div(B, 32), K);
+  if (cfg.gemm_dtype == LSAM_GEMM_BF16 || L.x3)
+    LAUNCH(c, LSAM_PROF_GATHER, launch_k(c, gather_t_kernel<bf16>, grid, dim3(32, 8), 0, xdst, nullptr, nullptr, rows, B, L.in0, L.ldb, c->at<bf16>(L.act[0]), nullptr, c->status(), nullptr, c->in_plane()));
+  else
+    LAUNCH(c, LSAM_PROF_GATHER, launch_k(c, gather_t_kernel<float>, grid, dim3(32, 8), 0, xdst, nullptr, nullptr, rows, B, L.in0, L.ldb, c->at<float>(L.act[0]), nullptr, c->status(), nullptr, (int64_t)0));
+  int rc = forward_pass(c);
+  if (rc == LSAM_OK) {
+    char why[256] = "";
+    int score_rc = LSAM_OK;
+    const int C = L.layers.back().out;
+    LAUNCH(c, LSAM_PROF_LOSS, score_rc = lsam_logprob(c->at<float>(L.logits), LSAM_FP32, K, B, C, (int64_t)C * L.ldb, 1, L.ldb, yb ? c->at<int32_t>(L.ylab) : nullptr, top_k, d_logp, d_lse,
+                                                      d_entropy, d_top_logp, d_top_idx, c->stream, why, sizeof why));
+    if (score_rc != LSAM_OK) rc = c->fail(score_rc, why);
+  }
+  if (c->async_on) LSAM_CUDA(c, cudaMemcpyAsync(c->active_buf(), kept, 4 * (size_t)K, cudaMemcpyDeviceToDevice, c->stream));
+  return rc;
 }
 
 int lsam_stage_batch(lsam_ctx* c, const float* xb, const void* yb, int on_host) {

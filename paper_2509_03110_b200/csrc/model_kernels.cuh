@@ -173,6 +173,20 @@ head_chunk_kernel(const T* __restrict__ a, int64_t a_sz, int ldb, int64_t a_plan
     if (f < out) dst[(int64_t)f * ldb] = acc[f];
 }
 
+// The logits of a narrow head alone (scoring; a gradient pass sums them in softmax_ce_kernel): the bias plus the chunks in ascending order.
+// grid (ceil(B / 128), out, K), block 128.
+template <typename T>
+__global__ void __launch_bounds__(128)
+narrow_logits_kernel(const float* __restrict__ part, int nparts, const T* __restrict__ bias, int64_t ld_p, int64_t p_plane, int B, int out, int ldb,
+                     float* __restrict__ logits) {
+  grid_dep_sync();
+  const int b = blockIdx.x * 128 + threadIdx.x, c = blockIdx.y, k = blockIdx.z;
+  if (b >= B) return;
+  float v = load_planes(bias + (int64_t)k * ld_p + c, p_plane);
+  for (int p = 0; p < nparts; ++p) v += part[(((int64_t)k * nparts + p) * kHeadMaxOut + c) * ldb + b];
+  logits[((int64_t)k * out + c) * ldb + b] = v;
+}
+
 // Backward through a narrow head (out <= kHeadMaxOut classes) into the layer below, with that layer's bias gradient:
 //   dh[i][b] = sum_c W[c][i] dz[c][b] (classes ascending);  dz_prev[i][b] = mask[i][b] ? T(dh) : 0;  dh_out = T(dh) (skip connections, nullable);
 //   db[i] = sum_b dz_prev[i][b] as stored -> g[z][b_off + i];  sum of squares of the block's 8 db -> partial[z][slot0 + blockIdx.x] (nullable).
