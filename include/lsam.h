@@ -363,11 +363,15 @@ int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t ro
 /* The first three results of lsam_logprob for the logits l = h w^T + bias, which are never stored:
  *  d_h [K, rows, inner] and d_w [K, classes, inner] of `dtype`, the inner index contiguous; w_stride_k = 0 shares one head among the workers.
  *  d_bias [K, classes] fp32 (bias_stride_k, 0 = shared) or NULL.  Labels and results as in lsam_logprob.
- * Products are accumulated in fp32.  16-bit operands whose addresses and strides are multiples of 16 bytes run on the tensor cores.
+ * Products are accumulated in fp32.  16-bit operands whose addresses and strides are multiples of 16 bytes go to the tensor cores as they are;
+ * others are first copied into the workspace (fp32 as three bf16 planes, whose six leading products keep fp32 accuracy), except small products and
+ * at most eight rows, which stay on the FMA pipes.
  *  d_workspace: lsam_head_logprob_workspace_bytes() bytes, 256-byte aligned, contents irrelevant before and after; calls that may overlap on
- *  the GPU (other streams, graphs replayed side by side) need one each.
+ *  the GPU (other streams, graphs replayed side by side) need one each.  flags of the query: LSAM_HEAD_ALIGNED = addresses and strides of h and w are
+ *  multiples of 16 bytes, LSAM_HEAD_SHARED = w_stride_k is 0.  The query is host-only and returns 0 for sizes that the call refuses.
  * K <= 65535, rows <= 4194240. */
-size_t lsam_head_logprob_workspace_bytes(int32_t K, int64_t rows, int64_t classes);
+enum { LSAM_HEAD_ALIGNED = 1, LSAM_HEAD_SHARED = 2 };
+size_t lsam_head_logprob_workspace_bytes(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, int32_t flags);
 int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
                       int64_t h_stride_k, int64_t h_stride_row, int64_t w_stride_k, int64_t w_stride_class, int64_t bias_stride_k,
                       const int32_t* d_labels, float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes,

@@ -114,7 +114,7 @@ def lib():
     L.lsam_logprob.argtypes = [vp, i32, i32] + [i64] * 5 + [vp, i32] + [vp] * 5 + err
     L.lsam_logprob_grad.argtypes = [vp, i32, i32] + [i64] * 5 + [vp] * 6 + [i64] * 3 + err
     L.lsam_head_logprob_workspace_bytes.restype = C.c_size_t
-    L.lsam_head_logprob_workspace_bytes.argtypes = [i32, i64, i64]
+    L.lsam_head_logprob_workspace_bytes.argtypes = [i32, i32, i64, i64, i64, i32]
     L.lsam_head_logprob.argtypes = [vp, vp, vp, i32, i32] + [i64] * 8 + [vp] * 5 + [C.c_size_t] + err
     L.lsam_dropout.argtypes = [vp, vp, vp, i32, i32] + [i64] * 8 + [C.c_double, C.c_uint64, C.c_uint64, i32, i32] + err
     _lib = L
@@ -172,6 +172,7 @@ def lsam_row_norms_static(g, n, out, stream=None):
 
 # ---- operators around a classifier's head (include/lsam.h, last section)
 FP32, BF16, FP16 = 0, 1, 2
+HEAD_ALIGNED, HEAD_SHARED = 1, 2
 TOP_MAX, DROPOUT_LAYERS, DROPOUT_WORKERS = 32, 4096, 1 << 20
 
 
@@ -193,7 +194,7 @@ def _invalid(msg):
 # operators allocate through an empty tensor of the right type and device, and ask for the stream's handle alone.
 _torch = _raw_stream = None
 _codes = {}  # torch dtype -> LSAM_FP32 / LSAM_BF16 / LSAM_FP16
-_protos = {}  # device -> (empty float32 tensor, empty int32 tensor): what results are allocated like; they hold no memory
+_protos = {}  # device -> empty float32 tensor: what results are allocated like; it holds no memory
 _err = threading.local()  # one message buffer per thread
 
 
@@ -213,7 +214,7 @@ def _load():
 def _proto(dev):
     p = _protos.get(dev)
     if p is None:
-        p = _protos[dev] = tuple(_torch.empty(0, dtype=t, device=dev) for t in (_torch.float32, _torch.int32))
+        p = _protos[dev] = _torch.empty(0, dtype=_torch.float32, device=dev)
     return p
 
 
@@ -276,16 +277,18 @@ def lsam_logprob(logits, labels=None, top_k=0, stream=None):
     dev = logits.device
     lead = logits.shape[:-1]
     pl = None if labels is None else _ptr(labels, "labels", lead, torch.int32, dev)
-    f32, i32 = _proto(dev)
-    lse = f32.new_empty(lead)
-    ent = torch.empty_like(lse)
-    logp = None if labels is None else torch.empty_like(lse)
+    f32 = _proto(dev)
+    if labels is None:
+        logp = None
+        lse, ent = f32.new_empty((2, *lead)).unbind(0)
+    else:
+        logp, lse, ent = f32.new_empty((3, *lead)).unbind(0)
     tv = ti = pv = pi = None
     if top_k:
         if not 0 < top_k <= TOP_MAX:
             raise _invalid(f"top_k outside 0 .. {TOP_MAX}")
-        shape = (*lead, top_k)
-        tv, ti = f32.new_empty(shape), i32.new_empty(shape)
+        tv, ti = f32.new_empty((2, *lead, top_k)).unbind(0)
+        ti = ti.view(torch.int32)
         pv, pi = tv.data_ptr(), ti.data_ptr()
     _call(lib().lsam_logprob, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, top_k, None if logp is None else logp.data_ptr(), lse.data_ptr(), ent.data_ptr(), pv, pi,
           _raw_stream(dev))
@@ -343,14 +346,19 @@ def lsam_head_logprob(h, w, labels=None, bias=None, stream=None):
     if bias is not None:
         pb = _ptr(bias, "bias", (V,) if bias.dim() == 1 else (K, V), torch.float32, dev)
         bk = V if bias.dim() == 2 else 0
-    f32 = _proto(dev)[0]
-    lse = f32.new_empty(lead)
-    ent = torch.empty_like(lse)
-    logp = None if labels is None else torch.empty_like(lse)
+    f32 = _proto(dev)
+    if labels is None:
+        logp = None
+        lse, ent = f32.new_empty((2, *lead)).unbind(0)
+    else:
+        logp, lse, ent = f32.new_empty((3, *lead)).unbind(0)
     L = lib()
-    nbytes = L.lsam_head_logprob_workspace_bytes(K, R, V)
+    ph, pw = h.data_ptr(), w.data_ptr()
+    unit = 3 if code == FP32 else 7  # elements of 16 bytes, minus one
+    aligned = not ((ph | pw) & 15) and not ((hk if K > 1 else 0) | (hr if R > 1 else 0) | (wk if K > 1 else 0) | (wc if V > 1 else 0)) & unit and (hr > 0 or R == 1) and (hk > 0 or K == 1) and (wc > 0 or V == 1)
+    nbytes = L.lsam_head_logprob_workspace_bytes(code, K, R, D, V, (HEAD_ALIGNED if aligned else 0) | (0 if wk else HEAD_SHARED)) if K and R else 0
     ws = f32.new_empty(nbytes // 4 + 64)
-    _call(L.lsam_head_logprob, h.data_ptr(), w.data_ptr(), pb, code, K, R, D, V, hk, hr, wk, wc, bk, pl, None if logp is None else logp.data_ptr(), lse.data_ptr(),
+    _call(L.lsam_head_logprob, ph, pw, pb, code, K, R, D, V, hk, hr, wk, wc, bk, pl, None if logp is None else logp.data_ptr(), lse.data_ptr(),
           ent.data_ptr(), (ws.data_ptr() + 255) // 256 * 256, nbytes, _raw_stream(dev))
     return LogProb(logp, lse, ent, None, None)
 
@@ -486,11 +494,10 @@ class Lsam:
         if int(np.prod(tuple(xb.shape[2:]))) != n_in:
             raise _invalid(f"a row of xb must hold {n_in} features")
         with torch.cuda.stream(self.stream):
-            f32, i32 = _proto(self.workspace.device)
-            lse = f32.new_empty((K, B))
-            ent = torch.empty_like(lse)
-            logp = None if yb is None else torch.empty_like(lse)
-            tv, ti = (f32.new_empty((K, B, top_k)), i32.new_empty((K, B, top_k))) if top_k else (None, None)
+            f32 = _proto(self.workspace.device)
+            logp, lse, ent = f32.new_empty((3, K, B)).unbind(0)
+            tv, ti = f32.new_empty((2, K, B, top_k)).unbind(0) if top_k else (None, None)
+            logp, ti = None if yb is None else logp, None if ti is None else ti.view(torch.int32)
         ptr = lambda a: None if a is None else C.c_void_p(a.data_ptr()) if isinstance(a, torch.Tensor) else _np_ptr(a)  # noqa: E731
         self._check(lib().lsam_score_batch(self._h, ptr(xb), ptr(yb), 1 if on_host else 0, top_k, ptr(logp), ptr(lse), ptr(ent), ptr(tv), ptr(ti)))
         return LogProb(logp, lse, ent, tv, ti)

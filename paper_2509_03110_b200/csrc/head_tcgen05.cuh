@@ -42,7 +42,9 @@ struct HeadTile {
   int a_rows;          // rows of h a load brings in (a multiple of 8, at most 128)
   int stages, stage_bytes, a_bytes;  // the ring: [h tile][w tile] per stage, each on a 1024-byte boundary
   int w_shared;        // one head for all workers
+  int pairs;           // 1, or 6: fp32 operands as three bf16 planes, plane p of worker k at index k + p K of the maps
   uint32_t idesc;
+  int K;
   int64_t units;       // K * runs * m_tiles
 };
 
@@ -74,6 +76,7 @@ __device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int6
   stat_add_all(st, l, mx);
 }
 
+// fp32 operands arrive as three bf16 planes each (head_copy_kernel) and six products of planes are accumulated, as in the fp32 models' GEMMs.
 // grid: CTAs (pairs: clusters of 2), each walking units u, u + grid, ...; unit = (run of class tiles, row tile) of a worker, row tile fastest
 template <bool PAIR>
 __global__ void __launch_bounds__(kHtThreads, 1)
@@ -93,7 +96,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
   const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
   const bool leader = rank == 0u;
   const int64_t unit = PAIR ? blockIdx.x / 2 : blockIdx.x, units = PAIR ? gridDim.x / 2 : gridDim.x;
-  const int k_blocks = (int)((a.inner + kHtK - 1) / kHtK), chunks = (k_blocks + kHtChunk - 1) / kHtChunk;
+  const int k_blocks = (int)((a.inner + kHtK - 1) / kHtK), k_total = q.pairs * k_blocks, chunks = (k_total + kHtChunk - 1) / kHtChunk;
   const int b_rows = PAIR ? q.tile_n / 2 : q.tile_n;  // classes staged by this CTA
   const uint32_t stage_tx = (uint32_t)(q.a_rows + b_rows) * kHtK * 2;
 
@@ -128,23 +131,26 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
         const int r0 = (mt * (PAIR ? 2 : 1) + (int)rank) * kHtRows, kw = q.w_shared ? 0 : k;
         const int nt_end = min(q.n_tiles, (rn + 1) * q.run);
         for (int nt = rn * q.run; nt < nt_end && ok; ++nt) {
-          const int k_first = PAIR ? 0 : (int)((int64_t)nt * k_blocks / q.n_tiles);
           const int c0 = nt * q.tile_n + (int)rank * b_rows;
-          for (int kq = 0; kq < k_blocks; ++kq) {
-            const int kb = kq + k_first < k_blocks ? kq + k_first : kq + k_first - k_blocks;
-            if (!tc::mbar_wait(&empty[s], ph ^ 1u, abort_flag)) { ok = false; break; }
-            uint8_t* dst = ring + s * STAGE;
-            if (PAIR) {
-              if (leader) tc::mbar_expect_tx(&full[s], 2 * stage_tx);
-              const uint32_t bar = tc::map_to_cta(tc::smem_u32(&full[s]), 0u);
-              tc::tma_load_3d_pair(dst, &map_h, kb * kHtK, r0, k, bar);
-              tc::tma_load_3d_pair(dst + A_BYTES, &map_w, kb * kHtK, c0, kw, bar);
-            } else {
-              tc::mbar_expect_tx(&full[s], stage_tx);
-              tc::tma_load_3d(dst, &map_h, kb * kHtK, r0, k, &full[s]);
-              tc::tma_load_3d(dst + A_BYTES, &map_w, kb * kHtK, c0, kw, &full[s]);
+          for (int pp = 0; pp < q.pairs && ok; ++pp) {
+            // plane pairs (0,2) (1,1) (2,0) (0,1) (1,0) (0,0): the small products first, the rest below 2^-24 of |h| |w| left out
+            const int pa = q.pairs == 1 ? 0 : pp < 3 ? pp : pp < 5 ? pp - 3 : 0, pb = q.pairs == 1 ? 0 : pp < 3 ? 2 - pp : pp < 5 ? 4 - pp : 0;
+            const int zh = k + pa * q.K, zw = q.w_shared ? pb : kw + pb * q.K;
+            for (int kb = 0; kb < k_blocks; ++kb) {
+              if (!tc::mbar_wait(&empty[s], ph ^ 1u, abort_flag)) { ok = false; break; }
+              uint8_t* dst = ring + s * STAGE;
+              if (PAIR) {
+                if (leader) tc::mbar_expect_tx(&full[s], 2 * stage_tx);
+                const uint32_t bar = tc::map_to_cta(tc::smem_u32(&full[s]), 0u);
+                tc::tma_load_3d_pair(dst, &map_h, kb * kHtK, r0, zh, bar);
+                tc::tma_load_3d_pair(dst + A_BYTES, &map_w, kb * kHtK, c0, zw, bar);
+              } else {
+                tc::mbar_expect_tx(&full[s], stage_tx);
+                tc::tma_load_3d(dst, &map_h, kb * kHtK, r0, zh, &full[s]);
+                tc::tma_load_3d(dst + A_BYTES, &map_w, kb * kHtK, c0, zw, &full[s]);
+              }
+              if (++s == STAGES) { s = 0; ph ^= 1u; }
             }
-            if (++s == STAGES) { s = 0; ph ^= 1u; }
           }
         }
       }
@@ -157,7 +163,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
       for (int64_t u = unit; u < q.units && ok; u += units) {
         const int rn = (int)((u / q.m_tiles) % q.runs), nt_end = min(q.n_tiles, (rn + 1) * q.run);
         for (int nt = rn * q.run; nt < nt_end && ok; ++nt) {
-          for (int kb = 0; kb < k_blocks; ++kb) {
+          for (int kb = 0; kb < k_total; ++kb) {
             const int in_chunk = kb % kHtChunk;
             if (in_chunk == 0 && !tc::mbar_wait(&acc_empty[as], aph ^ 1u, abort_flag)) { ok = false; break; }
             const uint32_t d = tmem_base + (uint32_t)as * kHtMaxN;
@@ -173,7 +179,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
             if (PAIR) tc::umma_commit_pair(&empty[s]);
             else tc::umma_commit(&empty[s]);
             if (++s == STAGES) { s = 0; ph ^= 1u; }
-            if (in_chunk == kHtChunk - 1 || kb == k_blocks - 1) {
+            if (in_chunk == kHtChunk - 1 || kb == k_total - 1) {
               if (PAIR) tc::umma_commit_pair(&acc_full[as]);
               else tc::umma_commit(&acc_full[as]);
               if (++as == 2) { as = 0; aph ^= 1u; }
@@ -313,12 +319,14 @@ inline bool ht_make_map(CUtensorMap* m, const T* base, uint64_t inner, uint64_t 
 
 // False (nothing launched): the operands' addresses or strides are not what TMA takes.  *e: the launch's error.
 template <typename T>
-inline bool ht_launch(const T* h, const T* w, HeadArgs a, int32_t K, HeadTile q, cudaStream_t stream, cudaError_t* e) {
+inline bool ht_launch(const T* h, const T* w, HeadArgs a, int32_t K, HeadTile q, int planes, bool shared, cudaStream_t stream, cudaError_t* e) {
   const bool pair = a.rows > kHtRows;
   CUtensorMap mh, mw;
-  q.w_shared = a.wk == 0 || K == 1;
-  if (!ht_make_map(&mh, h, a.inner, a.rows, K, a.hr, a.hk, (uint32_t)q.a_rows)) return false;
-  if (!ht_make_map(&mw, w, a.inner, a.classes, q.w_shared ? 1 : K, a.wr, a.wk, (uint32_t)(pair ? q.tile_n / 2 : q.tile_n))) return false;
+  q.w_shared = shared;
+  q.K = K;
+  q.pairs = planes == 3 ? 6 : 1;
+  if (!ht_make_map(&mh, h, a.inner, a.rows, (uint64_t)K * planes, a.hr, a.hk, (uint32_t)q.a_rows)) return false;
+  if (!ht_make_map(&mw, w, a.inner, a.classes, (uint64_t)(q.w_shared ? 1 : K) * planes, a.wr, a.wk, (uint32_t)(pair ? q.tile_n / 2 : q.tile_n))) return false;
   q.idesc = tc::instr_desc(pair ? 256 : 128, q.tile_n, false, false);
   if (!std::is_same<T, bf16>::value) q.idesc &= ~((1u << 7) | (1u << 10));  // operands f16 instead of bf16
   a.parts = 2 * q.runs;

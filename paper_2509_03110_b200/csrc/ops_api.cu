@@ -218,30 +218,82 @@ extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K,
 
 namespace {
 
-// SIMT form of a head call: enough shares of the classes to occupy the machine, none shorter than a tile.
-struct SimtPlan {
+// Forms of a head call, by sizes, type and alignment:
+//   TENSOR  16-bit operands that TMA takes as they are;
+//   GEMV    at most eight rows that TMA does not take (fp32, unaligned): straight from memory to the FMA pipes;
+//   COPY    anything else of at least 2^24 products: copied into aligned rows (fp32: three bf16 planes), then the tensor cores;
+//   TILES   the rest.
+// Measured (us): see DESIGN.
+enum HeadForm { HEAD_TENSOR, HEAD_GEMV, HEAD_COPY, HEAD_TILES };
+HeadForm head_form(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool aligned) {
+  if (dtype != LSAM_FP32 && aligned) return HEAD_TENSOR;
+  if (rows <= kGemvRows && gemv_smem(rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, inner) <= kGemvSmem) return HEAD_GEMV;
+  return (double)K * rows * inner * classes >= 16777216.0 ? HEAD_COPY : HEAD_TILES;
+}
+// GEMV and TILES: shares of the classes, enough to occupy the machine, none shorter than what a block takes at a time.
+struct SharePlan {
   int splits = 1;
   int64_t per_split = 0;
 };
-SimtPlan simt_plan(int32_t K, int64_t rows, int64_t classes) {
-  SimtPlan p;
-  const int64_t blocks = (int64_t)K * ceil_div(rows, kHsM);
-  const int64_t splits = std::min<int64_t>(ceil_div(2 * 148, blocks), ceil_div(classes, kHsN));
-  p.per_split = round_up(ceil_div(classes, splits), kHsN);
+SharePlan share_plan(HeadForm f, int32_t K, int64_t rows, int64_t classes) {
+  SharePlan p;
+  const int64_t least = f == HEAD_GEMV ? 64 : kHsN, blocks = (int64_t)K * (f == HEAD_GEMV ? 1 : ceil_div(rows, kHsM));
+  const int64_t splits = std::min<int64_t>(ceil_div(2 * 148, blocks), ceil_div(classes, least));
+  p.per_split = round_up(ceil_div(classes, splits), least);
   p.splits = (int)ceil_div(classes, p.per_split);
   return p;
 }
-// partial statistics of either form, then the labels' logits
-size_t head_part_bytes(int32_t K, int64_t rows, int64_t classes) {
-  const int64_t parts = std::max<int64_t>(simt_plan(K, rows, classes).splits, 2 * ht_plan(K, rows, classes).runs);
-  return (size_t)round_up((int64_t)sizeof(RowStat) * parts * K * rows, 256);
+// The workspace: partial statistics, the labels' logits, and in the COPY form the two matrices.
+struct HeadSpace {
+  size_t label, h, w, total;
+  int64_t pad;
+};
+HeadSpace head_space(HeadForm f, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool shared_w) {
+  const int64_t parts = f == HEAD_GEMV || f == HEAD_TILES ? share_plan(f, K, rows, classes).splits : 2 * ht_plan(K, rows, classes).runs;
+  const int64_t planes = dtype == LSAM_FP32 ? 3 : 1;
+  HeadSpace s;
+  s.pad = round_up(inner, 8);
+  s.label = (size_t)round_up((int64_t)sizeof(RowStat) * parts * K * rows, 256);
+  s.h = s.w = s.total = s.label + (size_t)round_up(4 * (int64_t)K * rows, 256);
+  if (f == HEAD_COPY) {
+    s.w = s.h + (size_t)round_up(2 * planes * K * rows * s.pad, 256);
+    s.total = s.w + (size_t)round_up(2 * planes * (shared_w ? 1 : K) * classes * s.pad, 256);
+  }
+  return s;
+}
+bool head_sizes_ok(int32_t K, int64_t rows, int64_t inner, int64_t classes) {
+  return K >= 1 && K <= 65535 && rows >= 1 && rows <= 4194240 && rows <= kMaxIndex / K && inner >= 1 && inner <= kMaxIndex && classes >= 1 && classes <= kMaxIndex;
+}
+
+template <typename T>
+cudaError_t launch_gemv(const T* h, const T* w, const HeadArgs& a, int32_t K, bool vec, cudaStream_t stream) {
+  const int R = a.rows <= 1 ? 1 : a.rows <= 2 ? 2 : a.rows <= 4 ? 4 : 8;
+  const int smem = (int)gemv_smem(R, a.inner);
+  const auto go = [&](auto kern) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemvSmem);
+    if (e != cudaSuccess) return e;
+    kern<<<dim3((unsigned)a.parts, 1, (unsigned)K), 256, smem, stream>>>(h, w, a);
+    return cudaPeekAtLastError();
+  };
+  const auto pick = [&](auto v) {
+    constexpr bool V = decltype(v)::value;
+    return R == 1 ? go(head_gemv_kernel<T, 1, V>) : R == 2 ? go(head_gemv_kernel<T, 2, V>) : R == 4 ? go(head_gemv_kernel<T, 4, V>) : go(head_gemv_kernel<T, 8, V>);
+  };
+  return vec ? pick(std::true_type()) : pick(std::false_type());
+}
+
+template <typename T, typename D>
+cudaError_t launch_copy(const T* src, int64_t sk, int64_t sr, int64_t Z, int64_t rows, int64_t inner, int64_t pad, D* dst, cudaStream_t stream) {
+  const int64_t cols = ceil_div(inner, 256), most = std::max<int64_t>(1, 148 * 32 / std::max<int64_t>(1, cols * Z));
+  head_copy_kernel<T, D><<<dim3((unsigned)cols, (unsigned)std::min<int64_t>({rows, most, 65535}), (unsigned)Z), 256, 0, stream>>>(src, sk, sr, rows, inner, pad, dst);
+  return cudaPeekAtLastError();
 }
 
 }  // namespace
 
-extern "C" size_t lsam_head_logprob_workspace_bytes(int32_t K, int64_t rows, int64_t classes) {
-  if (K < 1 || rows < 1 || classes < 1 || rows > kMaxIndex / K || classes > kMaxIndex) return 0;
-  return head_part_bytes(K, rows, classes) + 4 * (size_t)K * rows;
+extern "C" size_t lsam_head_logprob_workspace_bytes(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, int32_t flags) {
+  if (!dtype_ok(dtype) || !head_sizes_ok(K, rows, inner, classes)) return 0;
+  return head_space(head_form(dtype, K, rows, inner, classes, (flags & LSAM_HEAD_ALIGNED) != 0), dtype, K, rows, inner, classes, (flags & LSAM_HEAD_SHARED) != 0 || K == 1).total;
 }
 
 extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
@@ -254,34 +306,59 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
     return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= inner, classes < 2^31");
   if (d_logp && !d_labels) return err.fail(LSAM_ERR_INVALID, "d_logp without d_labels");
   if (K == 0 || rows == 0) return LSAM_OK;
-  if (K > 65535 || rows > kMaxIndex / K || rows > (int64_t)kHsM * 65535) return err.fail(LSAM_ERR_INVALID, "need K <= 65535, rows <= 4194240, K * rows < 2^31");
+  if (K > 65535 || rows > kMaxIndex / K || rows > 4194240) return err.fail(LSAM_ERR_INVALID, "need K <= 65535, rows <= 4194240, K * rows < 2^31");
   if (!strides_ok(K, h_stride_k, rows, h_stride_row, inner, 1) || !strides_ok(K, w_stride_k, classes, w_stride_class, inner, 1) || bias_stride_k < 0)
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
-  const int64_t total = (int64_t)K * rows;
-  const size_t part_bytes = head_part_bytes(K, rows, classes);
-  if (workspace_bytes < part_bytes + 4 * (size_t)total) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_head_logprob_workspace_bytes()");
+  const int64_t total = (int64_t)K * rows, es = (int64_t)dtype_size(dtype);
+  const bool shared = w_stride_k == 0 || K == 1;
+  const auto aligned16 = [&](const void* p, int64_t n0, int64_t s0, int64_t n1, int64_t s1) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (n0 == 1 || (s0 > 0 && s0 * es % 16 == 0)) && (n1 == 1 || (s1 > 0 && s1 * es % 16 == 0));
+  };
+  const bool h_aligned = aligned16(d_h, K, h_stride_k, rows, h_stride_row), w_aligned = aligned16(d_w, shared ? 1 : K, w_stride_k, classes, w_stride_class);
+  const HeadForm form = head_form(dtype, K, rows, inner, classes, h_aligned && w_aligned);
+  const HeadSpace sp = head_space(form, dtype, K, rows, inner, classes, shared);
+  if (workspace_bytes < sp.total) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_head_logprob_workspace_bytes()");
   if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return err.fail(LSAM_ERR_WORKSPACE, "workspace not 256-byte aligned");
   PtrCheck pc;
-  pc.need(d_h, dtype_size(dtype)); pc.need(d_w, dtype_size(dtype)); pc.need(d_workspace, 256);
+  pc.need(d_h, es); pc.need(d_w, es); pc.need(d_workspace, 256);
   pc.optional(d_bias, 4); pc.optional(d_labels, 4); pc.optional(d_logp, 4); pc.optional(d_lse, 4); pc.optional(d_entropy, 4);
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
+  char* ws = static_cast<char*>(d_workspace);
   HeadArgs a{rows, inner, classes, total, h_stride_k, h_stride_row, w_stride_k, w_stride_class, bias_stride_k, d_bias, d_labels, 0, 0,
-             static_cast<RowStat*>(d_workspace), reinterpret_cast<float*>(static_cast<char*>(d_workspace) + part_bytes)};
+             reinterpret_cast<RowStat*>(ws), reinterpret_cast<float*>(ws + sp.label)};
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     const T *h = static_cast<const T*>(d_h), *w = static_cast<const T*>(d_w);
-    if constexpr (sizeof(T) == 2) {
-      const HeadTile q = ht_plan(K, rows, classes);
-      a.parts = 2 * q.runs;
-      if (ht_launch(h, w, a, K, q, stream, &e)) return;
+    if (form == HEAD_GEMV || form == HEAD_TILES) {
+      const SharePlan p = share_plan(form, K, rows, classes);
+      a.parts = p.splits;
+      a.per_split = p.per_split;
+      if (form == HEAD_GEMV) {
+        e = launch_gemv<T>(h, w, a, K, w_aligned, stream);
+      } else {
+        head_score_simt_kernel<T><<<dim3((unsigned)p.splits, (unsigned)ceil_div(rows, kHsM), (unsigned)K), 256, 0, stream>>>(h, w, a);
+        e = cudaPeekAtLastError();
+      }
+      return;
     }
-    const SimtPlan p = simt_plan(K, rows, classes);
-    a.parts = p.splits;
-    a.per_split = p.per_split;
-    head_score_simt_kernel<T><<<dim3((unsigned)p.splits, (unsigned)ceil_div(rows, kHsM), (unsigned)K), 256, 0, stream>>>(h, w, a);
-    e = cudaPeekAtLastError();
+    const HeadTile q = ht_plan(K, rows, classes);
+    a.parts = 2 * q.runs;
+    if (form == HEAD_COPY) {
+      using D = typename std::conditional<sizeof(T) == 4, bf16, T>::type;
+      constexpr int planes = sizeof(T) == 4 ? 3 : 1;
+      D *hc = reinterpret_cast<D*>(ws + sp.h), *wc = reinterpret_cast<D*>(ws + sp.w);
+      const int64_t KW = shared ? 1 : K;
+      if ((e = launch_copy<T, D>(h, a.hk, a.hr, K, rows, inner, sp.pad, hc, stream)) != cudaSuccess) return;
+      if ((e = launch_copy<T, D>(w, a.wk, a.wr, KW, classes, inner, sp.pad, wc, stream)) != cudaSuccess) return;
+      a.hr = a.wr = sp.pad;
+      a.hk = rows * sp.pad;
+      a.wk = classes * sp.pad;
+      if (!ht_launch<D>(hc, wc, a, K, q, planes, shared, stream, &e)) e = cudaErrorInvalidValue;
+    } else if constexpr (sizeof(T) == 2) {
+      if (!ht_launch<T>(h, w, a, K, q, 1, shared, stream, &e)) e = cudaErrorInvalidValue;
+    }
   });
   if (e == cudaSuccess) {
     // programmatic dependent launch: the join's blocks become resident while the tiles drain and wait for them there

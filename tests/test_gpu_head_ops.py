@@ -290,7 +290,8 @@ def head_reference(h, w, bias, y):
     return out
 
 
-HEADS = [(1, 1, 8, 1), (1, 1, 64, 40), (2, 3, 40, 130), (1, 130, 72, 300), (3, 65, 100, 1000), (1, 257, 128, 1000), (2, 129, 264, 513), (1, 5, 1001, 77), (1, 300, 512, 5003), (2, 256, 96, 2048), (1, 2, 24, 20011)]
+HEADS = [(1, 1, 8, 1), (1, 1, 64, 40), (2, 3, 40, 130), (1, 130, 72, 300), (3, 65, 100, 1000), (1, 257, 128, 1000), (2, 129, 264, 513), (1, 5, 1001, 77), (1, 300, 512, 5003), (2, 256, 96, 2048), (1, 2, 24, 20011),
+         (2, 7, 1001, 3000), (1, 8, 6500, 300), (1, 1, 4100, 999), (3, 4, 257, 130), (2, 100, 1003, 777), (1, 150, 2050, 301)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
@@ -307,7 +308,9 @@ def test_head_scores(size, dtype):
     if C > 4:
         bias[:, 3] = NINF  # a masked class
     for ww, bb in ((w, None), (w, bias), (w[0], bias[0])):
+        ws = torch.cuda.memory_allocated()
         r = G.lsam_head_logprob(h, ww, y, bias=bb)
+        assert torch.cuda.memory_allocated() - ws < 1 << 20  # the workspace is given back
         t = head_reference(h, ww, bb, y)
         close(r.lse, t["lse"], t["lse_err"])
         close(r.entropy, t["entropy"], t["ent_err"])

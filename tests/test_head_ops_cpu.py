@@ -85,8 +85,13 @@ def test_error_buffer_is_optional():
 
 def test_workspace_bytes_grow_with_the_rows():
     f = G.lib().lsam_head_logprob_workspace_bytes
-    assert f(0, 1, 1) == 0 and f(1, 0, 1) == 0 and f(1, 1, 0) == 0
-    assert 0 < f(1, 1, 1) <= f(1, 4096, 32768) and f(32, 256, 1000) >= 32 * 256 * 16
+    assert f(1, 0, 1, 1, 1, 1) == 0 and f(1, 1, 0, 1, 1, 1) == 0 and f(1, 1, 1, 0, 1, 1) == 0 and f(1, 1, 1, 1, 0, 1) == 0 and f(3, 1, 1, 1, 1, 1) == 0 and f(1, 70000, 1, 1, 1, 1) == 0
+    assert 0 < f(1, 1, 1, 64, 1, 1) <= f(1, 1, 4096, 64, 32768, 1) and f(1, 32, 256, 4096, 1000, 1) >= 32 * 256 * 16
+    # what the tensor cores do not take as it is, is copied: 2 bytes an element, three planes for fp32, a shared head once
+    copy = f(1, 4, 300, 1001, 5003, 0) - f(1, 4, 300, 1001, 5003, 1)
+    assert copy >= 2 * 1008 * 4 * (300 + 5003) and f(0, 4, 300, 1001, 5003, 0) - f(1, 4, 300, 1001, 5003, 0) >= 4 * 1008 * 4 * (300 + 5003)
+    assert f(1, 4, 300, 1001, 5003, 0) - f(1, 4, 300, 1001, 5003, 2) >= 2 * 1008 * 3 * 5003
+    assert f(0, 1, 8, 4096, 32768, 1) < 1 << 20  # few rows are read where they are
 
 
 def test_binding_refuses_what_is_not_a_cuda_tensor_of_the_right_form():
