@@ -111,9 +111,9 @@ template <int N> __device__ inline float warp_sums(float (&v)[N], int lane) {
 constexpr int kGemvRows = 8, kGemvSmem = 200 * 1024;
 inline int64_t gemv_smem(int R, int64_t inner) { return (int64_t)R * round_up(inner, 256) * 4; }
 template <typename T, int R, bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
 head_gemv_kernel(const T* __restrict__ h, const T* __restrict__ w, HeadArgs a) {
-  constexpr int G = R == 8 ? 4 : 8, NV = R * G, N = VEC ? vec_n<T>() : 1;
+  constexpr int G = R == 8 || (VEC && R == 4) ? 4 : 8, NV = R * G, N = VEC ? vec_n<T>() : 1;
   extern __shared__ __align__(16) float hs[];  // [R][inner rounded up to 256]
   __shared__ float red[3][8][NV];
   grid_dep_launch();

@@ -8,7 +8,7 @@
 //   PAIR (more than 128 rows): two CTAs share 256 rows x tile_n classes (cta_group::2), each staging its own 128 rows of h and half the
 //     classes; what bounds a CTA is the rate at which it takes in operands, 32 KB per 256 x 256 x 64 block instead of 48.
 //   single CTA (up to 128 rows): the bytes of w bound it; only the rows that exist are loaded (the others' accumulator rows are never read).
-// tile_n, a multiple of 32 up to 256, is the width that loads all SMs evenly.  The work list has the row tile fastest: the CTAs that run together
+// tile_n, a multiple of 32 (single CTAs: 16) up to 256, is the width that loads all SMs evenly.  The work list has the row tile fastest: the CTAs that run together
 // read the same few tiles of w, so w crosses HBM once, whatever the number of row tiles.
 // All waits are bounded as in gemm_tcgen05.cuh; a CTA that gives up leaves NaN statistics for its rows.
 #pragma once
@@ -47,6 +47,61 @@ struct HeadTile {
   int K;
   int64_t units;       // K * runs * m_tiles
 };
+
+// What the issuing warps do per block of 64 inner indices has to stay below the 512 clocks of a 256-wide tile's products.  Barriers and operands are
+// addressed by 32-bit shared-memory addresses, and of a matrix descriptor (tc::smem_desc with leading offset 16, stride offset 1024) only the low word
+// changes.  The one thread that issues is chosen by elect.sync: tcgen05 instructions take uniform registers, and under a test of the lane number the
+// compiler, which cannot know that one thread is active, guards every one of them (475 clocks a block beside the products; 4096 x 4096 x 32768:
+// 937 -> 784 us).  A pair's warps walk their loops whole and elect at the instruction (707 us); single CTAs elect once (4 rows: 59 -> 54 us).
+__device__ inline bool ht_elect() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
+__device__ inline bool ht_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  for (uint32_t i = 0; i < tc::kSpinLimit; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((i & 1023u) == 1023u && *abort_flag) return false;
+  }
+  return false;
+}
+constexpr uint32_t kHtDescHi = 64u | (1u << 14) | (2u << 29);
+__device__ inline uint32_t ht_desc_lo(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | (1u << 16); }
+template <bool PAIR>
+__device__ inline void ht_mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  if (PAIR)
+    asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\nsetp.ne.b32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kHtDescHi) : "memory");
+  else
+    asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\nsetp.ne.b32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kHtDescHi) : "memory");
+}
+template <bool PAIR>
+__device__ inline void ht_commit(uint32_t bar) {
+  if (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <bool PAIR>
+__device__ inline void ht_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+  if (PAIR)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
 
 // The statistics of 32 logits of a row: classes c0 .. c0 + 31, of which `have` exist.  *at_label receives the label's logit.
 __device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int64_t c0, int have, const float* bias, int32_t y, float* at_label) {
@@ -122,10 +177,14 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHtRegsIssue));
-    if (warp == 0 && lane == 0) {
+    const bool one = ht_elect();
+    if (warp == 0 && (PAIR || one)) {
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
+      const uint32_t ring0 = tc::smem_u32(ring), full0 = tc::smem_u32(full), empty0 = tc::smem_u32(empty);
+      // both CTAs' loads of a stage complete on the leader's barrier, which the leader arms with the bytes of both
+      const uint32_t bar0 = PAIR ? tc::map_to_cta(full0, 0u) : full0, tx = PAIR ? 2 * stage_tx : stage_tx;
       for (int64_t u = unit; u < q.units && ok; u += units) {
         const int mt = (int)(u % q.m_tiles), rn = (int)((u / q.m_tiles) % q.runs), k = (int)(u / ((int64_t)q.m_tiles * q.runs));
         const int r0 = (mt * (PAIR ? 2 : 1) + (int)rank) * kHtRows, kw = q.w_shared ? 0 : k;
@@ -137,17 +196,12 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
             const int pa = q.pairs == 1 ? 0 : pp < 3 ? pp : pp < 5 ? pp - 3 : 0, pb = q.pairs == 1 ? 0 : pp < 3 ? 2 - pp : pp < 5 ? 4 - pp : 0;
             const int zh = k + pa * q.K, zw = q.w_shared ? pb : kw + pb * q.K;
             for (int kb = 0; kb < k_blocks; ++kb) {
-              if (!tc::mbar_wait(&empty[s], ph ^ 1u, abort_flag)) { ok = false; break; }
-              uint8_t* dst = ring + s * STAGE;
-              if (PAIR) {
-                if (leader) tc::mbar_expect_tx(&full[s], 2 * stage_tx);
-                const uint32_t bar = tc::map_to_cta(tc::smem_u32(&full[s]), 0u);
-                tc::tma_load_3d_pair(dst, &map_h, kb * kHtK, r0, zh, bar);
-                tc::tma_load_3d_pair(dst + A_BYTES, &map_w, kb * kHtK, c0, zw, bar);
-              } else {
-                tc::mbar_expect_tx(&full[s], stage_tx);
-                tc::tma_load_3d(dst, &map_h, kb * kHtK, r0, zh, &full[s]);
-                tc::tma_load_3d(dst + A_BYTES, &map_w, kb * kHtK, c0, zw, &full[s]);
+              if (!ht_wait(empty0 + 8 * s, ph ^ 1u, abort_flag)) { ok = false; break; }
+              const uint32_t dst = ring0 + s * STAGE;
+              if (!PAIR || one) {
+                if (!PAIR || leader) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full0 + 8 * s), "r"(tx) : "memory");
+                ht_load<PAIR>(dst, &map_h, kb * kHtK, r0, zh, bar0 + 8 * s);
+                ht_load<PAIR>(dst + A_BYTES, &map_w, kb * kHtK, c0, zw, bar0 + 8 * s);
               }
               if (++s == STAGES) { s = 0; ph ^= 1u; }
             }
@@ -156,32 +210,34 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
       }
       if (!ok) *abort_flag = 1;
     }
-    if (warp == 1 && lane == 0 && leader) {
+    if (warp == 1 && leader && (PAIR || one)) {
       int s = 0, as = 0;
       uint32_t ph = 0, aph = 0;
       bool ok = true;
+      const uint32_t full0 = tc::smem_u32(full), empty0 = tc::smem_u32(empty), acc_full0 = tc::smem_u32(acc_full), acc_empty0 = tc::smem_u32(acc_empty);
+      const uint32_t lo0 = ht_desc_lo(tc::smem_u32(ring)), step = (uint32_t)STAGE >> 4, b_off = (uint32_t)A_BYTES >> 4;
       for (int64_t u = unit; u < q.units && ok; u += units) {
         const int rn = (int)((u / q.m_tiles) % q.runs), nt_end = min(q.n_tiles, (rn + 1) * q.run);
         for (int nt = rn * q.run; nt < nt_end && ok; ++nt) {
+          int in_chunk = 0;
           for (int kb = 0; kb < k_total; ++kb) {
-            const int in_chunk = kb % kHtChunk;
-            if (in_chunk == 0 && !tc::mbar_wait(&acc_empty[as], aph ^ 1u, abort_flag)) { ok = false; break; }
-            const uint32_t d = tmem_base + (uint32_t)as * kHtMaxN;
-            if (!tc::mbar_wait(&full[s], ph, abort_flag)) { ok = false; break; }
-            tc::tc_fence_after();
-            const uint32_t pa = tc::smem_u32(ring + s * STAGE), pb = pa + A_BYTES;
-#pragma unroll
-            for (int k = 0; k < kHtK / 16; ++k) {
-              const uint64_t ad = tc::smem_desc(pa + k * 32, 16, 1024), bd = tc::smem_desc(pb + k * 32, 16, 1024);
-              if (PAIR) tc::umma_bf16_pair(d, ad, bd, q.idesc, (in_chunk | k) != 0 ? 1u : 0u);
-              else tc::umma_bf16(d, ad, bd, q.idesc, (in_chunk | k) != 0 ? 1u : 0u);
+            if (in_chunk == 0) {
+              if (!ht_wait(acc_empty0 + 8 * as, aph ^ 1u, abort_flag)) { ok = false; break; }
+              tc::tc_fence_after();
             }
-            if (PAIR) tc::umma_commit_pair(&empty[s]);
-            else tc::umma_commit(&empty[s]);
+            if (!ht_wait(full0 + 8 * s, ph, abort_flag)) { ok = false; break; }
+            const uint32_t d = tmem_base + (uint32_t)as * kHtMaxN, a_lo = lo0 + s * step, b_lo = a_lo + b_off;
+            const bool last = in_chunk == kHtChunk - 1 || kb == k_total - 1;
+            if (!PAIR || one) {
+#pragma unroll
+              for (int k = 0; k < kHtK / 16; ++k) ht_mma<PAIR>(d, a_lo + 2 * k, b_lo + 2 * k, q.idesc, in_chunk + k);  // 16 indices are 32 bytes along the row
+              ht_commit<PAIR>(empty0 + 8 * s);
+              if (last) ht_commit<PAIR>(acc_full0 + 8 * as);
+            }
             if (++s == STAGES) { s = 0; ph ^= 1u; }
-            if (in_chunk == kHtChunk - 1 || kb == k_total - 1) {
-              if (PAIR) tc::umma_commit_pair(&acc_full[as]);
-              else tc::umma_commit(&acc_full[as]);
+            ++in_chunk;
+            if (last) {
+              in_chunk = 0;
               if (++as == 2) { as = 0; aph ^= 1u; }
             }
           }
@@ -265,8 +321,8 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
 
 // ------------------------------------------------------------------------------------------------ host side
 // The width of a tile and the run of tiles that load the machine most evenly: the CTAs (pairs) work through ceil(units / CTAs) rounds of `run`
-// tiles; a tile costs its width plus the share of h it takes in (measured as 32 classes' worth).  Longer runs leave fewer partial statistics.
-// 32768 classes, 4 rows: 147 tiles of 224 instead of 128 of 256, so that every SM streams its share of w.
+// tiles.  A pair's tile costs its width plus the share of h it takes in (32 classes' worth); a single CTA's, whose bytes of w count, its width, plus a
+// little per tile and the last tile's statistics, which nothing hides.  Longer runs leave fewer partial statistics.
 inline HeadTile ht_plan(int32_t K, int64_t rows, int64_t classes) {
   // the search takes a few microseconds: the last one of a thread is kept, by its sizes
   struct Last { int32_t K = 0; int64_t rows = 0, classes = 0; HeadTile q{}; };
@@ -277,11 +333,13 @@ inline HeadTile ht_plan(int32_t K, int64_t rows, int64_t classes) {
   const int64_t ctas = pair ? 74 : 148;
   q.m_tiles = (int)ceil_div(rows, pair ? 2 * kHtRows : kHtRows);
   double best = 0.0;
-  for (int n = kHtMaxN; n >= 32; n -= 32) {
+  const int grain = pair ? 32 : 16;  // the multiple of 16 that tcgen05.mma wants, in each CTA of a pair
+  for (int n = kHtMaxN; n >= 32; n -= grain) {
     const int64_t n_tiles = ceil_div(classes, (int64_t)n);
     for (int64_t run = std::min<int64_t>(n_tiles, 32); run >= 1; --run) {
       const int64_t runs = ceil_div(n_tiles, run);
-      const double cost = (double)ceil_div((int64_t)K * q.m_tiles * runs, ctas) * run * (n + 32) * (1.0 + 0.02 / run);
+      const double tiles = (double)ceil_div((int64_t)K * q.m_tiles * runs, ctas) * run;
+      const double cost = (pair ? tiles * (n + 32) : tiles * (n + 8) + 0.25 * n) * (1.0 + 0.02 / run);
       if (best == 0.0 || cost < best) {
         best = cost;
         q.tile_n = n; q.run = (int)run; q.n_tiles = (int)n_tiles; q.runs = (int)runs;
