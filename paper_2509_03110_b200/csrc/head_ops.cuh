@@ -776,6 +776,56 @@ logprob_feature_kernel(LogitView<T> v, const int32_t* __restrict__ labels, Score
   if (lane < o.top_k) write_top(o, iw, lane, best[w][lane], sc);
 }
 
+// Many rows of few classes: a thread per row, 16 logits at a time; an alternative costs one more walk over the row, which is in L1 or L2.
+template <typename T>
+__global__ void __launch_bounds__(128)
+logprob_thread_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreOut o, uint32_t total) {
+  const uint32_t i = blockIdx.x * 128 + threadIdx.x;
+  if (i >= total) return;
+  const int32_t y = labels ? labels[i] : 0;
+  if (y < 0) {
+    write_left_out(o, i);
+    return;
+  }
+  const T* row = v.row(i);
+  RowStat a = stat_empty();
+  for (int32_t c0 = 0; c0 < v.classes; c0 += 16) {
+    float l[16], mx = kMasked;
+    const T* p = row + c0 * v.sc;
+#pragma unroll
+    for (int j = 0; j < 16; ++j, p += v.sc) l[j] = c0 + j < v.classes ? to_float(*p) : -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      l[j] = max_nan(l[j], kMasked);
+      mx = fmaxf(mx, l[j]);
+    }
+    stat_add_all(a, l, mx);
+  }
+  const RowScore sc = stat_finish(a);
+  write_scores(o, i, sc, y, v.classes, o.logp && y < v.classes ? to_float(row[y * v.sc]) : NAN);
+  float last = INFINITY;  // the previous alternative: the next one is the first largest behind it in (value, class) order
+  int32_t last_c = -1;
+  for (int k = 0; k < o.top_k; ++k) {
+    float best = kMasked;
+    int32_t best_c = -1;
+    if (k == 0 || last_c >= 0) {
+      for (int32_t c0 = 0; c0 < v.classes; c0 += 16) {
+        float l[16];
+        const T* p = row + c0 * v.sc;
+#pragma unroll
+        for (int j = 0; j < 16; ++j, p += v.sc) l[j] = c0 + j < v.classes ? to_float(*p) : -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (l[j] > best && (l[j] < last || (l[j] == last && c0 + j > last_c))) { best = l[j]; best_c = c0 + j; }
+      }
+    }
+    o.top_logp[(int64_t)i * o.top_k + k] = best_c >= 0 ? score_logp(best, sc) : -INFINITY;
+    o.top_idx[(int64_t)i * o.top_k + k] = best_c;
+    last = best;
+    last_c = best_c;
+  }
+}
+
 // Gradient of L(logp, entropy) of every row:  dl_c = a (1[c = y] - p_c) - b p_c (log p_c + H),  p_c = e^(l_c - lse),
 // a = dL/dlogp, b = dL/dH (each nullable = 0).  Rows that are left out (y < 0) or hold nothing but masks (lse = -inf) get 0.
 // With u = l - lse it is p (c0 + c1 u), c0 = -(a + b H), c1 = -b, plus a at the label: one read, one write, two multiply-adds and one exponential

@@ -92,13 +92,22 @@ cudaError_t launch_row(const LogitView<T>& v, const int32_t* labels, const Score
   return cudaLaunchKernelEx(&cfg, logprob_row_kernel<T, NT, CS>, v, labels, out);
 }
 
-// Which form a call takes.  Sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 1024 classes, 128 threads
-// up to 32 KB, 256 beyond; rows of 32 KB and more that leave most of the machine idle are split over a cluster of 8 or 4 blocks
-// (4 rows of 131072 bf16, 8 alternatives: 14.4 us with one block a row, 8.3 with eight; 64 rows: 14.4, four blocks 10.7).
+// Which form a call takes.  Many rows of few classes: a thread per row, from 32768 rows of up to 256 classes with the sample index contiguous (106647
+// rows of 95 bf16: 87 us in the feature kernel, 10 with a thread per row; 5 alternatives 41), from 4096 rows of up to 64 contiguous classes (60000 rows
+// of 10 fp32: 5 us), unless the alternatives, a walk over the row each, cost more (8192 rows of 64, 8 alternatives: 47 us against a warp's 20).  Other
+// sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 1024 classes, 128 threads up to 32 KB, 256 beyond;
+// rows of 32 KB and more that leave most of the machine idle are split over a cluster of 8 or 4 blocks (4 rows of 131072 bf16, 8 alternatives: 14.4 us
+// with one block a row, 8.3 with eight; 64 rows: 14.4, four blocks 10.7).
 template <typename T>
 cudaError_t launch_scores(const LogitView<T>& v, const int32_t* labels, const ScoreOut& out, int32_t K, cudaStream_t stream) {
   const int64_t total = (int64_t)K * v.rows;
-  if (v.sc != 1 && v.sr == 1 && v.rows > 1) {
+  const bool samples = v.sc != 1 && v.sr == 1 && v.rows > 1;
+  const int64_t walks = (int64_t)out.top_k * v.classes;
+  if (samples ? total >= 32768 && v.classes <= 256 && walks <= 512 : total >= 4096 && v.classes <= 64 && (out.top_k <= 1 || walks <= 160)) {
+    logprob_thread_kernel<T><<<(unsigned)ceil_div(total, 128), 128, 0, stream>>>(v, labels, out, (uint32_t)total);
+    return cudaPeekAtLastError();
+  }
+  if (samples) {
     const int64_t row_blocks = ceil_div(v.rows, feat_rows<T>());
     logprob_feature_kernel<T><<<(unsigned)(K * row_blocks), feat_rows<T>() * kFeatG, 0, stream>>>(v, labels, out, (uint32_t)row_blocks);
     return cudaPeekAtLastError();

@@ -120,6 +120,21 @@ def test_scores(size, layout, dtype):
     check_scores(l, None, 3)
 
 
+@pytest.mark.parametrize("layout, rows, C", [("row", 5000, 10), ("row", 4097, 64), ("feature", 33000, 17), ("feature", 40000, 100), ("feature", 32768, 256), ("strided", 4100, 33)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_scores_of_many_short_rows(layout, rows, C, dtype):
+    l = make_logits(1, rows, C, dtype, layout, seed=C, pad=C % 3)
+    l[0, 1] = NINF
+    l[0, 2, ::2] = NINF
+    l[0, 3] = 0.0
+    l[0, 4, C // 2] = NAN
+    l[0, 5] = torch.finfo(DT[dtype]).min if dtype != "fp16" else NINF
+    y = make_labels(1, rows, C, C)
+    y[0, 0], y[0, rows - 1], y[0, 6] = -1, -7, C
+    for k in (0, 1, 5, 32):
+        check_scores(l, y, k)
+
+
 @pytest.mark.parametrize("layout", ["row", "feature"])
 @pytest.mark.parametrize("C", [10, 257, 1000, 4100, 40001])
 def test_scores_of_masked_rows(C, layout):
