@@ -232,7 +232,8 @@ namespace {
 //   GEMV    at most eight rows that TMA does not take (fp32, unaligned): straight from memory to the FMA pipes;
 //   COPY    anything else of at least 2^24 products: copied into aligned rows (fp32: three bf16 planes), then the tensor cores;
 //   TILES   the rest.
-// Measured (us): see DESIGN.
+// Measured (us): 2048 x 1021 x 16384 bf16 in fp32 tiles 2847, copied 92; 1000 x 1000 x 4096 fp32 in tiles 225, in planes 72; 4 x 4096 x 32768 fp32 in tiles
+// 287, GEMV 102; 16 x 100 x 1000 fp32 in tiles 12, two copies more than the product itself.
 enum HeadForm { HEAD_TENSOR, HEAD_GEMV, HEAD_COPY, HEAD_TILES };
 HeadForm head_form(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool aligned) {
   if (dtype != LSAM_FP32 && aligned) return HEAD_TENSOR;
