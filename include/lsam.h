@@ -352,9 +352,9 @@ int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, i
  *   dlogits[c] = dlogp (1[c = label] - p_c) - dentropy p_c (log p_c + entropy),   p_c = e^(l[c] - lse)
  * with lse and entropy [K, rows] as lsam_logprob returned them for the same logits, dlogp and dentropy [K, rows] the loss's derivatives
  * (nullable: 0; not both NULL; dlogp needs d_labels, dentropy needs d_entropy).  The minibatch cross-entropy of a context is
- * dlogp = -1 / batch.  Rows that are left out (negative label) and rows of nothing but
- * masks (lse = -inf) get zeros; a label >= classes makes its row NaN.
- * d_dlogits: type of the logits, strides of its own (no two elements at one address); may be d_logits itself with the same strides. */
+ * dlogp = -1 / batch.  Rows that are left out (negative label) and rows of nothing but masks (lse = -inf) get zeros, whatever else they
+ * hold; in any other row a label >= classes makes the row NaN.
+ * d_dlogits: type of the logits, strides of its own (every dimension steps over all that the smaller strides span); may be d_logits itself with the same strides. */
 int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                       int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
                       const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
@@ -365,11 +365,13 @@ int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t ro
  *  d_bias [K, classes] fp32 (bias_stride_k, 0 = shared) or NULL.  Labels and results as in lsam_logprob.
  * Products are accumulated in fp32.  16-bit operands whose addresses and strides are multiples of 16 bytes go to the tensor cores as they are;
  * others are first copied into the workspace (fp32 as three bf16 planes, whose six leading products keep fp32 accuracy), except small products and
- * at most eight rows, which stay on the FMA pipes.
+ * at most eight rows, which stay on the FMA pipes.  Classes are masked through the bias: an fp32 element of h or w that is infinite, or above 3.38e38,
+ * the largest bf16, may turn the logits it enters into NaN.
  *  d_workspace: lsam_head_logprob_workspace_bytes() bytes, 256-byte aligned, contents irrelevant before and after; calls that may overlap on
- *  the GPU (other streams, graphs replayed side by side) need one each.  flags of the query: LSAM_HEAD_ALIGNED = addresses and strides of h and w are
- *  multiples of 16 bytes, LSAM_HEAD_SHARED = w_stride_k is 0.  The query is host-only and returns 0 for sizes that the call refuses.
- * K <= 65535, rows <= 4194240. */
+ *  the GPU (other streams, graphs replayed side by side) need one each.  flags of the query: LSAM_HEAD_ALIGNED = addresses of h and w and
+ *  the strides of their dimensions of more than one element are multiples of 16 bytes, and none of them 0 but w_stride_k; LSAM_HEAD_SHARED =
+ *  w_stride_k is 0.  The query is host-only and returns 0 for sizes that the call refuses.
+ * K <= 65535, rows <= 4194240, inner and classes <= 2^30. */
 enum { LSAM_HEAD_ALIGNED = 1, LSAM_HEAD_SHARED = 2 };
 size_t lsam_head_logprob_workspace_bytes(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, int32_t flags);
 int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
@@ -385,7 +387,7 @@ int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int
  * gives the 16-bit numbers of eight columns (word (c mod 8) / 2, low half first); a column is dropped when its number is below
  * cut = floor(65536 p + 1/2), and scale = 65536 / (65536 - cut), so p is used to the nearest 2^-16 and the expectation is exact for it.
  * Dropped elements are not multiplied: a NaN there gives 0.  p = 1 drops everything.
- * out may be x or skip itself with the same strides; the rows of out must not overlap otherwise. */
+ * out may be x or skip itself with the same strides, else it must overlap neither; its rows must not overlap or interleave. */
 #define LSAM_DROPOUT_LAYERS 4096
 #define LSAM_DROPOUT_WORKERS 1048576
 int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, int32_t dtype, int32_t K, int64_t rows, int64_t n, int64_t x_stride_k,

@@ -232,6 +232,8 @@ def _stacked(t, what):
     """K, rows, columns and the strides of a [rows, columns] or [K, rows, columns] tensor."""
     n = t.dim()
     if n == 3:
+        if t.shape[0] >> 31:
+            raise _invalid(f"{what}: 2^31 workers or more")
         return (*t.shape, *t.stride())
     if n == 2:
         return (1, *t.shape, 0, *t.stride())
@@ -377,6 +379,8 @@ def lsam_dropout(x, p, seed, tick, layer=0, k_offset=0, skip=None, out=None, str
     dev = x.device
     if not 0 <= seed < 1 << 64 or not 0 <= tick < 1 << 64:
         raise _invalid("seed and tick are unsigned 64-bit numbers")
+    if not 0 <= layer < DROPOUT_LAYERS or not 0 <= k_offset < DROPOUT_WORKERS:
+        raise _invalid(f"layer outside 0 .. {DROPOUT_LAYERS - 1} or k_offset outside 0 .. {DROPOUT_WORKERS - 1}")
     if out is None:
         out = x.new_empty(x.shape)
     elif out.shape != x.shape or out.dtype != x.dtype or out.device != dev:
@@ -478,6 +482,7 @@ class Lsam:
         """Log probability of the labels, log-sum-exp, entropy and top_k alternatives of a minibatch under every worker's iterate.
 
         xb [K, B, in] float32, yb [K, B] int32 or None: both CUDA tensors, or both host tensors / numpy arrays.  Returns LogProb of CUDA tensors [K, B].
+        Runs on the context's stream: other streams order their reads of the result behind it, and it behind what produced xb and yb.
         """
         torch = _load()
         if not 0 <= top_k <= TOP_MAX:
@@ -500,6 +505,10 @@ class Lsam:
             logp, ti = None if yb is None else logp, None if ti is None else ti.view(torch.int32)
         ptr = lambda a: None if a is None else C.c_void_p(a.data_ptr()) if isinstance(a, torch.Tensor) else _np_ptr(a)  # noqa: E731
         self._check(lib().lsam_score_batch(self._h, ptr(xb), ptr(yb), 1 if on_host else 0, top_k, ptr(logp), ptr(lse), ptr(ent), ptr(tv), ptr(ti)))
+        if not on_host:  # their memory is not handed out again before the context's stream has read it
+            for t in (xb, yb):
+                if t is not None:
+                    t.record_stream(self.stream)
         return LogProb(logp, lse, ent, tv, ti)
 
     def should_couple(self):

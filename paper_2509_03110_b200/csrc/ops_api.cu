@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdio>
 #include <type_traits>
+#include <utility>
 
 #include "common.cuh"
 #include "dropout.cuh"
@@ -62,13 +63,26 @@ struct PtrCheck {
   }
 };
 
-constexpr int64_t kMaxIndex = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxIndex = ((int64_t)1 << 31) - 1, kMaxHead = (int64_t)1 << 30;
 
 // extents n0 x n1 x n2 with element strides s0, s1, s2: every offset fits a signed 64-bit byte count
 bool strides_ok(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2) {
   if (s0 < 0 || s1 < 0 || s2 < 0) return false;
   const __int128 last = (__int128)(n0 - 1) * s0 + (__int128)(n1 - 1) * s1 + (__int128)(n2 - 1) * s2;
   return last < ((__int128)1 << 60);
+}
+
+// No two elements at one address: in the order of their strides, every dimension steps over all that the smaller ones span.
+bool disjoint(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2) {
+  std::pair<int64_t, int64_t> d[3] = {{s0, n0}, {s1, n1}, {s2, n2}};
+  std::sort(d, d + 3);
+  __int128 span = 1;
+  for (const auto& e : d) {
+    if (e.second <= 1) continue;
+    if (e.first < span) return false;
+    span += (__int128)e.first * (e.second - 1);
+  }
+  return true;
 }
 
 template <class F>
@@ -207,8 +221,7 @@ extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K,
   if (rows > kMaxIndex / K) return err.fail(LSAM_ERR_INVALID, "K * rows must be below 2^31");
   if (!strides_ok(K, stride_k, rows, stride_row, classes, stride_class) || !strides_ok(K, out_stride_k, rows, out_stride_row, classes, out_stride_class))
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or the tensor is too large");
-  if ((K > 1 && out_stride_k == 0) || (rows > 1 && out_stride_row == 0) || (classes > 1 && out_stride_class == 0))
-    return err.fail(LSAM_ERR_INVALID, "elements of the gradient share an address");
+  if (!disjoint(K, out_stride_k, rows, out_stride_row, classes, out_stride_class)) return err.fail(LSAM_ERR_INVALID, "elements of the gradient share an address or interleave");
   PtrCheck pc;
   pc.need(d_logits, dtype_size(dtype)); pc.need(d_dlogits, dtype_size(dtype)); pc.need(d_lse, 4);
   pc.optional(d_labels, 4); pc.optional(d_entropy, 4); pc.optional(d_dlogp, 4); pc.optional(d_dentropy, 4);
@@ -230,7 +243,8 @@ namespace {
 // Forms of a head call, by sizes, type and alignment:
 //   TENSOR  16-bit operands that TMA takes as they are;
 //   GEMV    at most eight rows that TMA does not take (fp32, unaligned): straight from memory to the FMA pipes;
-//   COPY    anything else of at least 2^24 products: copied into aligned rows (fp32: three bf16 planes), then the tensor cores;
+//   COPY    anything else of at least 2^24 products, or of more rows than a grid of TILES has: copied into aligned rows (fp32: three bf16 planes),
+//           then the tensor cores;
 //   TILES   the rest.
 // Measured (us): 2048 x 1021 x 16384 bf16 in fp32 tiles 2847, copied 92; 1000 x 1000 x 4096 fp32 in tiles 225, in planes 72; 4 x 4096 x 32768 fp32 in tiles
 // 287, GEMV 102; 16 x 100 x 1000 fp32 in tiles 12, two copies more than the product itself.
@@ -238,7 +252,7 @@ enum HeadForm { HEAD_TENSOR, HEAD_GEMV, HEAD_COPY, HEAD_TILES };
 HeadForm head_form(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool aligned) {
   if (dtype != LSAM_FP32 && aligned) return HEAD_TENSOR;
   if (rows <= kGemvRows && gemv_smem(rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, inner) <= kGemvSmem) return HEAD_GEMV;
-  return (double)K * rows * inner * classes >= 16777216.0 ? HEAD_COPY : HEAD_TILES;
+  return (double)K * rows * inner * classes >= 16777216.0 || rows > 65535 * (int64_t)kHsM ? HEAD_COPY : HEAD_TILES;
 }
 // GEMV and TILES: shares of the classes, enough to occupy the machine, none shorter than what a block takes at a time.
 struct SharePlan {
@@ -272,7 +286,7 @@ HeadSpace head_space(HeadForm f, int32_t dtype, int32_t K, int64_t rows, int64_t
   return s;
 }
 bool head_sizes_ok(int32_t K, int64_t rows, int64_t inner, int64_t classes) {
-  return K >= 1 && K <= 65535 && rows >= 1 && rows <= 4194240 && rows <= kMaxIndex / K && inner >= 1 && inner <= kMaxIndex && classes >= 1 && classes <= kMaxIndex;
+  return K >= 1 && K <= 65535 && rows >= 1 && rows <= 4194240 && rows <= kMaxIndex / K && inner >= 1 && inner <= kMaxHead && classes >= 1 && classes <= kMaxHead;
 }
 
 template <typename T>
@@ -312,12 +326,12 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
                                  void* cuda_stream, char* h_err, size_t h_err_len) {
   const Err err("lsam_head_logprob", h_err, h_err_len);
   if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
-  if (K < 0 || rows < 0 || inner < 1 || classes < 1 || classes > kMaxIndex || inner > kMaxIndex)
-    return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= inner, classes < 2^31");
+  if (K < 0 || rows < 0 || inner < 1 || classes < 1 || classes > kMaxHead || inner > kMaxHead)
+    return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= inner, classes <= 2^30");
   if (d_logp && !d_labels) return err.fail(LSAM_ERR_INVALID, "d_logp without d_labels");
   if (K == 0 || rows == 0) return LSAM_OK;
   if (K > 65535 || rows > kMaxIndex / K || rows > 4194240) return err.fail(LSAM_ERR_INVALID, "need K <= 65535, rows <= 4194240, K * rows < 2^31");
-  if (!strides_ok(K, h_stride_k, rows, h_stride_row, inner, 1) || !strides_ok(K, w_stride_k, classes, w_stride_class, inner, 1) || bias_stride_k < 0)
+  if (!strides_ok(K, h_stride_k, rows, h_stride_row, inner, 1) || !strides_ok(K, w_stride_k, classes, w_stride_class, inner, 1) || !strides_ok(K, bias_stride_k, classes, 1, 1, 0))
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
   const int64_t total = (int64_t)K * rows, es = (int64_t)dtype_size(dtype);
   const bool shared = w_stride_k == 0 || K == 1;
@@ -424,7 +438,7 @@ extern "C" int lsam_dropout(const void* d_x, const void* d_skip, void* d_out, in
   if (!strides_ok(K, x_stride_k, rows, x_stride_row, n, 1) || !strides_ok(K, out_stride_k, rows, out_stride_row, n, 1) ||
       (d_skip && !strides_ok(K, skip_stride_k, rows, skip_stride_row, n, 1)))
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
-  if ((K > 1 && out_stride_k == 0) || (rows > 1 && out_stride_row < n)) return err.fail(LSAM_ERR_INVALID, "elements of the output share an address");
+  if (!disjoint(K, out_stride_k, rows, out_stride_row, n, 1)) return err.fail(LSAM_ERR_INVALID, "elements of the output share an address or interleave");
   if ((__int128)ceil_div(n, 256) * rows * K > kMaxIndex) return err.fail(LSAM_ERR_INVALID, "K * rows * ceil(n / 256) must be below 2^31");
   PtrCheck pc;
   pc.need(d_x, dtype_size(dtype)); pc.need(d_out, dtype_size(dtype)); pc.optional(d_skip, dtype_size(dtype));

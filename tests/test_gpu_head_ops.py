@@ -175,6 +175,22 @@ def test_alternatives_of_tied_and_sorted_rows(C, dtype):
         check_scores(l.transpose(1, 2).contiguous().transpose(1, 2), None, k)
 
 
+@pytest.mark.parametrize("K, rows", [(2, 17), (1, 3), (2, 32), (1, 148)])  # rows split over eight blocks and over four
+@pytest.mark.parametrize("dtype, C", [("fp32", 20011), ("bf16", 33001)])
+def test_ties_and_masks_in_split_rows(K, rows, dtype, C):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    l = torch.randint(-3, 3, (K, rows, C), generator=g, device="cuda").to(DT[dtype])
+    l[0, 0] = NINF
+    l[0, 1] = NINF; l[0, 1, C - 3:] = 2.0
+    l[0, 2] = -1.0
+    l[K - 1, rows - 1, ::2] = torch.finfo(DT[dtype]).min
+    l[K - 1, 0, C // 2] = NAN if K > 1 else 9.0
+    y = make_labels(K, rows, C, 1)
+    y[0, 1], y[K - 1, 2] = C - 1, -1
+    for k in (0, 1, 9, 32):
+        check_scores(l, y, k)
+
+
 def test_scores_beyond_32_bit_offsets():
     stride = (1 << 31) + 8
     C = 1000
@@ -266,6 +282,23 @@ def test_gradient_into_other_strides_and_in_place():
     assert torch.equal(l, want)
 
 
+def test_gradient_of_empty_rows_and_expanded_logits():
+    for C in (33, 2000):
+        l = torch.full((1, 3, C), NINF, device="cuda")
+        l[0, 2] = 0.5
+        y = torch.tensor([[C, 1, C]], device="cuda", dtype=torch.int32)
+        r = G.lsam_logprob(l, y)
+        for t in (l, l.transpose(1, 2).contiguous().transpose(1, 2)):
+            d = G.lsam_logprob_grad(t, y, r.lse, torch.ones_like(r.lse))
+            assert not d[0, :2].any() and torch.isnan(d[0, 2]).all()  # nothing but masks comes before a label that is no class
+        base = torch.randn((1, 1, C), generator=torch.Generator(device="cuda").manual_seed(C), device="cuda")
+        e = base.expand(2, 5, C)
+        y = make_labels(2, 5, C, C)
+        r = check_scores(e, y, 3)
+        want, tol = grad_reference(e, y, r.lse, r.entropy, torch.ones_like(r.lse), None)
+        close(G.lsam_logprob_grad(e, y, r.lse, torch.ones_like(r.lse)), want, tol)
+
+
 def test_gradient_against_differences():
     # of the 64-bit loss sum a logp + b entropy, along random directions: a central difference of step h is off by h^2 / 6 |L'''| <= 1e-9 here
     l = make_logits(1, 6, 50, "fp32", "row", seed=9, scale=1.0)
@@ -351,6 +384,39 @@ def test_head_scores_of_strided_and_masked_operands():
         h[1, 2, 0] = INF
         r = G.lsam_head_logprob(h, w, y)
         assert torch.isnan(r.lse[0, 1]) and not torch.isfinite(r.lse[1, 2]) and torch.isfinite(r.lse[0, 2:]).all() and torch.isfinite(r.lse[1, 3:]).all()
+
+
+def check_head(h, w, y, bias=None):
+    r = G.lsam_head_logprob(h, w, y, bias=bias)
+    t = head_reference(h, w, bias, y)
+    close(r.lse, t["lse"], t["lse_err"])
+    close(r.entropy, t["entropy"], t["ent_err"])
+    close(r.logp, t["logp"], t["lse_err"] + t["l_err"] + 4 * U * torch.nan_to_num(t["logp"], 0, 0, 0).abs())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 5, 70, 200])
+def test_head_scores_of_permuted_and_expanded_operands(rows, dtype):
+    K, C, D = 3, 300, 136
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    h, w = rand(K, rows, D).to(DT[dtype]), (rand(K, C, D) / 8).to(DT[dtype])
+    y = make_labels(K, rows, C, rows)
+    hp, wp = h.transpose(0, 1).contiguous().transpose(0, 1), w.transpose(0, 1).contiguous().transpose(0, 1)  # the workers' stride below the rows'
+    check_head(hp, wp, y)
+    check_head(h, wp, y, bias=rand(K, C))
+    check_head(h[:1].expand(K, rows, D), w, y)               # one batch for all workers
+    check_head(h[:, :1].expand(K, rows, D), w[0], y)         # one row, read again
+    check_head(h, w[:, :1].expand(K, C, D), y)               # every class the same
+    check_head(h, w[:1].expand(K, C, D), y, bias=rand(C))    # a shared head as an expanded tensor
+    flat = (rand(C * 8 + D) / 8).to(DT[dtype])
+    check_head(h, flat.as_strided((C, D), (8, 1)), y)        # classes whose rows overlap
+
+
+def test_head_scores_of_more_rows_than_a_grid_of_tiles():
+    g = torch.Generator(device="cuda").manual_seed(0)
+    rows = 65535 * 32 + 40
+    check_head(torch.randn((1, rows, 2), generator=g, device="cuda"), torch.randn((3, 2), generator=g, device="cuda"), make_labels(1, rows, 3, 0))
 
 
 def test_head_scores_agree_with_scores_of_stored_logits():
@@ -467,6 +533,8 @@ def test_refusals_on_the_device():
         lambda: G.lsam_logprob_grad(l, y, r.lse, r.lse, out=l[:, :1].expand(1, 4, 100)), lambda: G.lsam_logprob_grad(l, y, r.lse, r.lse, out=l.bfloat16()),
         lambda: G.lsam_head_logprob(l, l.bfloat16()), lambda: G.lsam_head_logprob(l, l[:, :, :50]), lambda: G.lsam_head_logprob(l, l.transpose(1, 2).contiguous().transpose(1, 2)),
         lambda: G.lsam_dropout(l.transpose(1, 2), 0.5, 1, 1), lambda: G.lsam_dropout(l, 0.5, 1, 1, skip=l[:, :2]), lambda: G.lsam_dropout(l, 2.0, 1, 1), lambda: G.lsam_dropout(l, 0.5, 1, 1, out=l[:, :1].expand(1, 4, 100)),
+        lambda: G.lsam_dropout(l, 0.5, 1, 1, layer=1 << 32), lambda: G.lsam_dropout(l, 0.5, 1, 1, k_offset=1 << 32),  # would wrap in a 32-bit argument
+        lambda: G.lsam_logprob_grad(l, y, r.lse, r.lse, out=torch.zeros(200, device="cuda").as_strided((1, 4, 100), (0, 3, 1))),
     ]
     for f in bad:
         with pytest.raises(G.LsamError) as e:

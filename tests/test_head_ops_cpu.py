@@ -42,15 +42,15 @@ def test_logprob_refuses(kw, word):
 
 @pytest.mark.parametrize("kw, word", [
     (dict(dtype=7), "dtype"), (dict(classes=0), "classes"), (dict(dlogp=None, dentropy=None), "neither"), (dict(labels=None), "d_labels"), (dict(entropy=None), "d_entropy"),
-    (dict(sc=-1), "stride"), (dict(orow=-1), "stride"), (dict(orow=0), "address"), (dict(oc=0), "address"), (dict(K=2, ok=0), "address"), (dict(K=1 << 16, rows=1 << 16), "2^31")])
+    (dict(sc=-1), "stride"), (dict(orow=-1), "stride"), (dict(orow=0), "address"), (dict(oc=0), "address"), (dict(K=2, ok=0), "address"), (dict(orow=4), "address"), (dict(K=2, ok=9), "address"), (dict(K=2, ok=1, orow=5), "address"), (dict(K=1 << 16, rows=1 << 16), "2^31")])
 def test_grad_refuses(kw, word):
     rc, msg = _grad(**kw)
     assert rc == G.LSAM_ERR_INVALID and word in msg, (rc, msg)
 
 
 @pytest.mark.parametrize("kw, code, word", [
-    (dict(dtype=5), G.LSAM_ERR_INVALID, "dtype"), (dict(inner=0), G.LSAM_ERR_INVALID, "inner"), (dict(classes=0), G.LSAM_ERR_INVALID, "classes"), (dict(labels=None), G.LSAM_ERR_INVALID, "d_labels"),
-    (dict(K=65536), G.LSAM_ERR_INVALID, "65535"), (dict(rows=4194241), G.LSAM_ERR_INVALID, "4194240"), (dict(hr=-8), G.LSAM_ERR_INVALID, "stride"), (dict(bk=-1), G.LSAM_ERR_INVALID, "stride"),
+    (dict(dtype=5), G.LSAM_ERR_INVALID, "dtype"), (dict(inner=0), G.LSAM_ERR_INVALID, "inner"), (dict(classes=(1 << 30) + 1), G.LSAM_ERR_INVALID, "2^30"), (dict(inner=(1 << 30) + 1), G.LSAM_ERR_INVALID, "2^30"), (dict(classes=0), G.LSAM_ERR_INVALID, "classes"), (dict(labels=None), G.LSAM_ERR_INVALID, "d_labels"),
+    (dict(K=65536), G.LSAM_ERR_INVALID, "65535"), (dict(rows=4194241), G.LSAM_ERR_INVALID, "4194240"), (dict(hr=-8), G.LSAM_ERR_INVALID, "stride"), (dict(bk=-1), G.LSAM_ERR_INVALID, "stride"), (dict(K=2, bk=1 << 61), G.LSAM_ERR_INVALID, "stride"),
     (dict(nbytes=4), G.LSAM_ERR_WORKSPACE, "workspace"), (dict(ws=C.c_void_p((1 << 20) + 16)), G.LSAM_ERR_WORKSPACE, "aligned")])
 def test_head_refuses(kw, code, word):
     rc, msg = _head(**kw)
@@ -59,7 +59,7 @@ def test_head_refuses(kw, code, word):
 
 @pytest.mark.parametrize("kw, word", [
     (dict(dtype=3), "dtype"), (dict(p=-0.1), "p outside"), (dict(p=1.01), "p outside"), (dict(p=float("nan")), "p outside"), (dict(n=-1), "negative"), (dict(layer=-1), "layer"), (dict(layer=4096), "layer"),
-    (dict(k_offset=-1), "workers"), (dict(k_offset=(1 << 20) - 1, K=2), "workers"), (dict(n=1 << 31), "2^31"), (dict(xr=-1), "stride"), (dict(orow=4), "address"), (dict(K=2, ok=0), "address"),
+    (dict(k_offset=-1), "workers"), (dict(k_offset=(1 << 20) - 1, K=2), "workers"), (dict(n=1 << 31), "2^31"), (dict(xr=-1), "stride"), (dict(orow=4), "address"), (dict(K=2, ok=0), "address"), (dict(K=2, ok=1), "address"), (dict(K=2, ok=7), "address"),
     (dict(rows=(1 << 31) - 1, n=(1 << 31) - 1, orow=(1 << 31) - 1, xr=0), "stride|2^31")])
 def test_dropout_refuses(kw, word):
     rc, msg = _dropout(**kw)
@@ -92,6 +92,7 @@ def test_workspace_bytes_grow_with_the_rows():
     assert copy >= 2 * 1008 * 4 * (300 + 5003) and f(0, 4, 300, 1001, 5003, 0) - f(1, 4, 300, 1001, 5003, 0) >= 4 * 1008 * 4 * (300 + 5003)
     assert f(1, 4, 300, 1001, 5003, 0) - f(1, 4, 300, 1001, 5003, 2) >= 2 * 1008 * 3 * 5003
     assert f(0, 1, 8, 4096, 32768, 1) < 1 << 20  # few rows are read where they are
+    assert f(0, 1, 65535 * 32 + 1, 1, 1, 0) - f(0, 1, 65535 * 32, 1, 1, 0) >= 3 * 2 * 8 * 65535 * 32  # more row tiles than a grid has: copied
 
 
 def test_binding_refuses_what_is_not_a_cuda_tensor_of_the_right_form():
@@ -105,3 +106,5 @@ def test_binding_refuses_what_is_not_a_cuda_tensor_of_the_right_form():
             G.lsam_logprob(bad)
     with pytest.raises(G.LsamError):
         G.lsam_dropout(x, 0.5, -1, 1)
+    with pytest.raises(G.LsamError, match="workers"):  # would wrap in a 32-bit argument
+        G.lsam_logprob(torch.zeros(1, 1, 1).expand(1 << 32, 1, 1))
