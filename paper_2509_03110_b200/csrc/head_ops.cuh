@@ -929,7 +929,7 @@ grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, FastDiv by_chunks, uin
 // Logits and gradient with the sample index contiguous: a thread owns R consecutive rows (a 16-byte vector, or one row where the strides do
 // not allow it) and 8 classes of a block's 64.  block (32, 8), grid K * row blocks * class blocks.
 template <typename T, int R>
-__global__ void __launch_bounds__(256, R == 8 ? 3 : 4)
+__global__ void __launch_bounds__(256, R == 8 ? 3 : R == 1 ? 5 : 4)
 grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_blocks, uint32_t class_blocks) {
   const uint32_t cb = blockIdx.x % class_blocks, kr = blockIdx.x / class_blocks, rb = kr % row_blocks, k = kr / row_blocks;
   const int64_t r0 = ((int64_t)rb * 32 + threadIdx.x) * R;
@@ -966,12 +966,22 @@ grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_block
         }
     }
   } else {
-    for (int e = 0; e < 8; ++e) {
-      const int64_t c = c0 + 8 * e;
-      if (c >= v.classes) break;
+    if constexpr (R == 1) {  // all loads in flight before the first store
+      T x[8];
 #pragma unroll
-      for (int j = 0; j < R; ++j)
-        if (r0 + j < v.rows) dst[c * out.sc + j] = from_float<T>(row[j](to_float(src[c * v.sc + j]), (int32_t)c));
+      for (int e = 0; e < 8; ++e)
+        if (c0 + 8 * e < v.classes) x[e] = src[(c0 + 8 * e) * v.sc];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c0 + 8 * e < v.classes) dst[(c0 + 8 * e) * out.sc] = from_float<T>(row[0](to_float(x[e]), (int32_t)c0 + 8 * e));
+    } else {  // the last rows
+      for (int e = 0; e < 8; ++e) {
+        const int64_t c = c0 + 8 * e;
+        if (c >= v.classes) break;
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+          if (r0 + j < v.rows) dst[c * out.sc + j] = from_float<T>(row[j](to_float(src[c * v.sc + j]), (int32_t)c));
+      }
     }
   }
 }

@@ -40,18 +40,30 @@ head_score_simt_kernel(const T* __restrict__ h, const T* __restrict__ w, HeadArg
     const int64_t r = r0 + ty * 2 + i;
     y[i] = (a.labels && r < a.rows) ? a.labels[k * a.rows + r] : -1;
   }
+  T x[10];  // 32 + 128 rows of 16, consecutive threads along the inner index: the next step's elements are on their way while this one's are used
+  auto fetch = [&](int64_t c0, int64_t d0) {
+#pragma unroll
+    for (int q = 0; q < 10; ++q) {
+      const int e = q * 256 + tid, rr = e >> 4;
+      const int64_t d = d0 + (e & 15), r = q < 2 ? r0 + rr : c0 + rr - kHsM;
+      x[q] = from_float<T>(0.f);
+      if (d < a.inner && r < (q < 2 ? a.rows : c_end)) x[q] = q < 2 ? hp[r * a.hr + d] : wp[r * a.wr + d];
+    }
+  };
+  fetch(c_begin, 0);
   for (int64_t c0 = c_begin; c0 < c_end; c0 += kHsN) {
     float acc[2][8] = {};
     for (int64_t d0 = 0; d0 < a.inner; d0 += kHsK) {
       __syncthreads();
 #pragma unroll
-      for (int q = 0; q < 10; ++q) {  // 32 + 128 rows of 16, consecutive threads along the inner index
+      for (int q = 0; q < 10; ++q) {
         const int e = q * 256 + tid, dd = e & 15, rr = e >> 4;
-        const bool in = d0 + dd < a.inner;
-        if (q < 2) hs[dd][rr] = in && r0 + rr < a.rows ? to_float(hp[(r0 + rr) * a.hr + d0 + dd]) : 0.f;
-        else wsm[dd][rr - kHsM] = in && c0 + rr - kHsM < c_end ? to_float(wp[(c0 + rr - kHsM) * a.wr + d0 + dd]) : 0.f;
+        if (q < 2) hs[dd][rr] = to_float(x[q]);
+        else wsm[dd][rr - kHsM] = to_float(x[q]);
       }
       __syncthreads();
+      if (d0 + kHsK < a.inner) fetch(c0, d0 + kHsK);
+      else if (c0 + kHsN < c_end) fetch(c0 + kHsN, 0);
 #pragma unroll
       for (int d = 0; d < kHsK; ++d) {
         const float4 b0 = *reinterpret_cast<const float4*>(&wsm[d][tx * 4]), b1 = *reinterpret_cast<const float4*>(&wsm[d][64 + tx * 4]);
@@ -198,28 +210,50 @@ head_gemv_kernel(const T* __restrict__ h, const T* __restrict__ w, HeadArgs a) {
   }
 }
 
-// Copies a matrix [K][rows][inner] of any strides into rows of `pad` elements (a multiple of 8) that TMA takes.  fp32 is split into three bf16 planes
-// p0 = bf16(x), p1 = bf16(x - p0), p2 = bf16(x - p0 - p1), [3][K][rows][pad], whose sum is x; 16-bit types keep theirs.  Consecutive lanes move consecutive
-// elements.  grid (ceil(inner / 256), min(rows, ..), K): a block walks rows blockIdx.y, + gridDim.y, ...
+// Copies h and w, [Z][rows][inner] of any strides, into rows of `pad` elements (a multiple of 8) that TMA takes, in one launch.  fp32 is split into three
+// bf16 planes p0 = bf16(x), p1 = bf16(x - p0), p2 = bf16(x - p0 - p1), [3][Z][rows][pad], whose sum is x; 16-bit types keep theirs.  `lanes` (a power of
+// two) consecutive threads move consecutive elements of a row; a block walks the rows, kCopyRows of a thread in flight.
+// grid h.blocks + w.blocks, block 256; a side's blocks: column block fastest, then row block, then worker
+constexpr int kCopyRows = 4;
+struct CopySide {
+  const void* src;
+  void* dst;
+  int64_t sk, sr, rows, Z;
+  uint32_t row_blocks, blocks;
+};
 template <typename T, typename D>
-__global__ void __launch_bounds__(256)
-head_copy_kernel(const T* __restrict__ src, int64_t sk, int64_t sr, int64_t rows, int64_t inner, int64_t pad, D* __restrict__ dst) {
-  const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x, k = blockIdx.z;
+__global__ void __launch_bounds__(256, 8)
+head_copy_kernel(CopySide h, CopySide w, int64_t inner, int64_t pad, int lanes, uint32_t cols) {
+  constexpr int U = kCopyRows;
+  const bool first = blockIdx.x < h.blocks;
+  const CopySide a = first ? h : w;
+  const uint32_t b = first ? blockIdx.x : blockIdx.x - h.blocks;
+  const int64_t d = (int64_t)(b % cols) * lanes + (threadIdx.x & (lanes - 1)), k = b / cols / a.row_blocks;
   if (d >= inner) return;
-  const int64_t plane = (int64_t)gridDim.z * rows * pad;
-  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
-    const T x = src[k * sk + r * sr + d];
-    D* p = dst + (k * rows + r) * pad + d;
-    if constexpr (sizeof(T) == 4) {
-      float f = to_float(x);
+  const int group = 256 / lanes;
+  const int64_t plane = a.Z * a.rows * pad, step = (int64_t)a.row_blocks * group;
+  const T* src = static_cast<const T*>(a.src) + k * a.sk + d;
+  D* dst = static_cast<D*>(a.dst) + k * a.rows * pad + d;
+  for (int64_t r = (int64_t)(b / cols % a.row_blocks) * group + threadIdx.x / lanes; r < a.rows; r += U * step) {
+    T x[U];
 #pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        const D v = from_float<D>(f);
-        p[q * plane] = v;
-        f -= to_float(v);
+    for (int u = 0; u < U; ++u)
+      if (r + u * step < a.rows) x[u] = src[(r + u * step) * a.sr];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (r + u * step >= a.rows) break;
+      D* p = dst + (r + u * step) * pad;
+      if constexpr (sizeof(T) == 4) {
+        float f = to_float(x[u]);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+          const D v = from_float<D>(f);
+          p[q * plane] = v;
+          f -= to_float(v);
+        }
+      } else {
+        *p = x[u];
       }
-    } else {
-      *p = x;
     }
   }
 }

@@ -122,13 +122,13 @@ __device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int6
       asm("{\n.reg .pred p;\nsetp.eq.s32 p, %1, %2;\n@p mov.f32 %0, %3;\n}\n" : "+f"(lab) : "r"((int)at), "r"(j), "f"(l[j]));
     *at_label = lab;
   }
-  float mx = st.m;
+  float mx[4] = {st.m, st.m, st.m, st.m};  // four chains
 #pragma unroll
   for (int j = 0; j < 32; ++j) {
     l[j] = max_nan(l[j], kMasked);
-    mx = fmaxf(mx, l[j]);
+    mx[j & 3] = fmaxf(mx[j & 3], l[j]);
   }
-  stat_add_all(st, l, mx);
+  stat_add_all(st, l, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
 }
 
 // fp32 operands arrive as three bf16 planes each (head_copy_kernel) and six products of planes are accumulated, as in the fp32 models' GEMMs.
@@ -269,15 +269,25 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
           if (!tc::mbar_wait(&acc_full[as], aph, abort_flag)) { ok = false; break; }
           tc::tc_fence_after();
           const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)as * kHtMaxN;
+          if (ch == 0) {  // all of them in flight at once
 #pragma unroll
-          for (int b = 0; b < kHtBlocks; ++b) {
-            const int c = (2 * b + half) * 32;
-            if (c < nv) {
-              uint32_t raw[32];
-              tc::tmem_ld32(taddr + (uint32_t)c, raw);
-              tc::tmem_ld_wait();
+            for (int b = 0; b < kHtBlocks; ++b)
+              if ((2 * b + half) * 32 < nv) tc::tmem_ld32(taddr + (uint32_t)(2 * b + half) * 32, l[b]);
+            tc::tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) l[b][j] = ch == 0 ? __uint_as_float(raw[j]) : l[b][j] + __uint_as_float(raw[j]);
+            for (int b = 0; b < kHtBlocks; ++b) tc::tmem_ld_arrived(l[b]);
+          } else {
+#pragma unroll
+            for (int b = 0; b < kHtBlocks; ++b) {
+              const int c = (2 * b + half) * 32;
+              if (c < nv) {
+                float more[32];
+                tc::tmem_ld32(taddr + (uint32_t)c, more);
+                tc::tmem_ld_wait();
+                tc::tmem_ld_arrived(more);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) l[b][j] += more[j];
+              }
             }
           }
           tc::tc_fence_before();

@@ -243,17 +243,13 @@ namespace {
 // Forms of a head call, by sizes, type and alignment:
 //   TENSOR  16-bit operands that TMA takes as they are;
 //   GEMV    at most eight rows that TMA does not take (fp32, unaligned): straight from memory to the FMA pipes;
-//   COPY    anything else of at least 2^24 products, or of more rows than a grid of TILES has: copied into aligned rows (fp32: three bf16 planes),
-//           then the tensor cores;
-//   TILES   the rest.
-// Measured (us): 2048 x 1021 x 16384 bf16 in fp32 tiles 2847, copied 92; 1000 x 1000 x 4096 fp32 in tiles 225, in planes 72; 4 x 4096 x 32768 fp32 in tiles
-// 287, GEMV 102; 16 x 100 x 1000 fp32 in tiles 12, two copies more than the product itself.
+//   TILES   small products: at most kTileSteps steps of kHsK inner indices for every SM's blocks;
+//   COPY    the rest: copied into aligned rows (fp32: three bf16 planes), then the tensor cores.
+// A step of TILES takes 0.8 to 1.7 us, whatever the rows; COPY has one launch more and moves both matrices.  Measured (us, TILES / COPY), bf16 rows x inner x
+// classes: 16 x 20 x 1000 7.4 / 8.9, 300 x 20 x 1000 7.7 / 11.2, 16 x 101 x 70 11.8 / 8.1, 82 x 301 x 1000 24 / 10.7, 82 x 1091 x 70 70 / 11.7, 2000 x 1021 x 16384
+// 4297 / 98;  fp32: 40 x 8 x 20001 12 / 33, 101 x 394 x 1722 31 / 19.8;  4 x 4096 x 32768 fp32 in tiles 287, GEMV 102.
 enum HeadForm { HEAD_TENSOR, HEAD_GEMV, HEAD_COPY, HEAD_TILES };
-HeadForm head_form(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool aligned) {
-  if (dtype != LSAM_FP32 && aligned) return HEAD_TENSOR;
-  if (rows <= kGemvRows && gemv_smem(rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, inner) <= kGemvSmem) return HEAD_GEMV;
-  return (double)K * rows * inner * classes >= 16777216.0 || rows > 65535 * (int64_t)kHsM ? HEAD_COPY : HEAD_TILES;
-}
+constexpr int64_t kTileSteps = 4;
 // GEMV and TILES: shares of the classes, enough to occupy the machine, none shorter than what a block takes at a time.
 struct SharePlan {
   int splits = 1;
@@ -266,6 +262,13 @@ SharePlan share_plan(HeadForm f, int32_t K, int64_t rows, int64_t classes) {
   p.per_split = round_up(ceil_div(classes, splits), least);
   p.splits = (int)ceil_div(classes, p.per_split);
   return p;
+}
+HeadForm head_form(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool aligned) {
+  if (dtype != LSAM_FP32 && aligned) return HEAD_TENSOR;
+  if (rows <= kGemvRows && gemv_smem(rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, inner) <= kGemvSmem) return HEAD_GEMV;
+  const SharePlan p = share_plan(HEAD_TILES, K, rows, classes);
+  const int64_t waves = ceil_div(K * ceil_div(rows, kHsM) * p.splits, 2 * 148);
+  return waves * ceil_div(p.per_split, kHsN) * ceil_div(inner, kHsK) <= kTileSteps ? HEAD_TILES : HEAD_COPY;
 }
 // The workspace: partial statistics, the labels' logits, and in the COPY form the two matrices.
 struct HeadSpace {
@@ -306,10 +309,23 @@ cudaError_t launch_gemv(const T* h, const T* w, const HeadArgs& a, int32_t K, bo
   return vec ? pick(std::true_type()) : pick(std::false_type());
 }
 
+// The widest group of lanes that leaves few of them idle at the end of a row.
 template <typename T, typename D>
-cudaError_t launch_copy(const T* src, int64_t sk, int64_t sr, int64_t Z, int64_t rows, int64_t inner, int64_t pad, D* dst, cudaStream_t stream) {
-  const int64_t cols = ceil_div(inner, 256), most = std::max<int64_t>(1, 148 * 32 / std::max<int64_t>(1, cols * Z));
-  head_copy_kernel<T, D><<<dim3((unsigned)cols, (unsigned)std::min<int64_t>({rows, most, 65535}), (unsigned)Z), 256, 0, stream>>>(src, sk, sr, rows, inner, pad, dst);
+cudaError_t launch_copy(CopySide h, CopySide w, int64_t inner, int64_t pad, cudaStream_t stream) {
+  int lanes = 256;
+  while (lanes > 8 && (lanes >= 2 * inner || (lanes > 32 && round_up(inner, lanes) * 7 > inner * 8))) lanes /= 2;
+  const int64_t cols = ceil_div(inner, lanes), group = 256 / lanes;
+  int64_t blocks = 0;
+  for (CopySide* s : {&h, &w}) {
+    // no more blocks than occupy the machine four times, unless columns and workers alone are more
+    const int64_t row_blocks = std::min(ceil_div(s->rows, group * kCopyRows), std::max<int64_t>(1, 148 * 32 / (cols * s->Z))), n = cols * row_blocks * s->Z;
+    if (n > kMaxIndex) return cudaErrorInvalidConfiguration;
+    s->row_blocks = (uint32_t)row_blocks;
+    s->blocks = (uint32_t)n;
+    blocks += n;
+  }
+  if (blocks > kMaxIndex) return cudaErrorInvalidConfiguration;
+  head_copy_kernel<T, D><<<(unsigned)blocks, 256, 0, stream>>>(h, w, inner, pad, lanes, (uint32_t)cols);
   return cudaPeekAtLastError();
 }
 
@@ -373,9 +389,8 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
       using D = typename std::conditional<sizeof(T) == 4, bf16, T>::type;
       constexpr int planes = sizeof(T) == 4 ? 3 : 1;
       D *hc = reinterpret_cast<D*>(ws + sp.h), *wc = reinterpret_cast<D*>(ws + sp.w);
-      const int64_t KW = shared ? 1 : K;
-      if ((e = launch_copy<T, D>(h, a.hk, a.hr, K, rows, inner, sp.pad, hc, stream)) != cudaSuccess) return;
-      if ((e = launch_copy<T, D>(w, a.wk, a.wr, KW, classes, inner, sp.pad, wc, stream)) != cudaSuccess) return;
+      e = launch_copy<T, D>({h, hc, a.hk, a.hr, rows, K, 0, 0}, {w, wc, a.wk, a.wr, classes, shared ? 1 : K, 0, 0}, inner, sp.pad, stream);
+      if (e != cudaSuccess) return;
       a.hr = a.wr = sp.pad;
       a.hk = rows * sp.pad;
       a.wk = classes * sp.pad;
