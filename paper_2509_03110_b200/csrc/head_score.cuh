@@ -213,7 +213,7 @@ head_gemv_kernel(const T* __restrict__ h, const T* __restrict__ w, HeadArgs a) {
 // Copies h and w, [Z][rows][inner] of any strides, into rows of `pad` elements (a multiple of 8) that TMA takes, in one launch.  fp32 is split into three
 // bf16 planes p0 = bf16(x), p1 = bf16(x - p0), p2 = bf16(x - p0 - p1), [3][Z][rows][pad], whose sum is x; 16-bit types keep theirs.  `lanes` (a power of
 // two) consecutive threads move consecutive elements of a row; a block walks the rows, kCopyRows of a thread in flight.
-// Bound by the bytes and, for 16-bit elements moved one by one, by issue.  Measured (us of the whole call): 2000 x 1021 x 16384 bf16 95 (one row in flight and
+// Bound by the bytes and, for 16-bit elements moved one by one, by issue.  Measured (us of the whole call): 2000 x 1021 x 16384 bf16 96 (one row in flight and
 // a launch for each matrix 98), 16 x 1091 x 1000 13.9 (17.4), 4 x 128 x 1078 x 3688 fp32 93 (94); eight rows in flight 118, 16.4, 100.
 // grid h.blocks + w.blocks, block 256; a side's blocks: column block fastest, then row block, then worker
 constexpr int kCopyRows = 4;
