@@ -22,7 +22,8 @@
 
 namespace lsam {
 
-// warp 0: TMA producer, warp 1: MMA issuer and tensor-memory owner, warps 2, 3: none; warps 4-11: draining.  A draining thread holds the 128
+// warp 0: TMA producer, warp 1: MMA issuer and tensor-memory owner, warps 2, 3: none; warps 4-11: draining (sixteen draining warps of half the
+// logits each are slower: 2 x 353 x 135 x 32546 fp32 131 -> 171 us).  A draining thread holds the 128
 // logits of its row's half tile, so the registers go to those two warpgroups: 56 + 2 x 216 a thread out of the 3 x 168 of the launch.
 constexpr int kHtThreads = 384;
 constexpr int kHtRegsIssue = 56, kHtRegsDrain = 216;
@@ -34,7 +35,8 @@ constexpr int kHtBlocks = kHtMaxN / 64;  // blocks of 32 classes a draining warp
 // are added in registers.
 constexpr int kHtChunk = 12;
 constexpr int kHtMaxStages = 12, kHtRing = 216 * 1024;  // bytes of the ring
-constexpr int kHtSmem = kHtRing + 1024 + 512;
+constexpr int kHtBiasBytes = 8 * kHtBlocks * 32 * 4;  // a tile's bias, per draining warp
+constexpr int kHtSmem = kHtRing + 1024 + 512 + kHtBiasBytes;
 
 struct HeadTile {
   int tile_n, run;     // classes of a tile, consecutive tiles of a unit of work
@@ -103,11 +105,14 @@ __device__ inline void ht_load(uint32_t dst, const CUtensorMap* map, int c0, int
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
 }
 
-// The statistics of 32 logits of a row: classes c0 .. c0 + 31, of which `have` exist.  *at_label receives the label's logit.
+// The statistics of 32 logits of a row: classes c0 .. c0 + 31, of which `have` exist.  bias: their 32 values in shared memory, or null.  *at_label receives the label's logit.
 __device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int64_t c0, int have, const float* bias, int32_t y, float* at_label) {
   if (bias != nullptr) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) l[j] += __ldg(bias + c0 + min(j, have - 1));
+    for (int q = 0; q < 8; ++q) {
+      const float4 v = reinterpret_cast<const float4*>(bias)[q];
+      l[4 * q] += v.x; l[4 * q + 1] += v.y; l[4 * q + 2] += v.z; l[4 * q + 3] += v.w;
+    }
   }
   if (have < 32) {
 #pragma unroll
@@ -145,7 +150,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
   uint64_t* acc_empty = acc_full + 2;    // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * kHtMaxStages + 4) * 8 + 8 <= 512, "barrier area");
+  static_assert((2 * kHtMaxStages + 4) * 8 + 8 <= 512 && kHtSmem <= 227 * 1024, "barrier area");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? tc::cluster_ctarank() : 0u;
@@ -248,6 +253,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kHtRegsDrain));
     const int quad = warp & 3, half = (warp - 4) >> 2;
+    float* my_bias = reinterpret_cast<float*>(ring + kHtRing + 512) + (warp - 4) * (kHtBlocks * 32);
     const uint32_t acc_empty_leader[2] = {PAIR ? tc::map_to_cta(tc::smem_u32(&acc_empty[0]), 0u) : 0u, PAIR ? tc::map_to_cta(tc::smem_u32(&acc_empty[1]), 0u) : 0u};
     int as = 0;
     uint32_t aph = 0;
@@ -265,6 +271,14 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
         const int64_t c_tile = (int64_t)nt * q.tile_n;
         const int nv = (int)min((int64_t)q.tile_n, a.classes - c_tile);  // classes that exist
         float l[kHtBlocks][32];  // this warp's blocks of 32 classes: half, half + 2, ...
+        // The bias of these classes, a value a lane, is asked for while the products run and read by all lanes from shared memory, four at a time: as 32
+        // loads of the same address by all lanes it cost as much as the statistics (2048 x 512 x 32768 with bias: 96 us, now 74).
+        float bv[kHtBlocks];
+#pragma unroll
+        for (int b = 0; b < kHtBlocks; ++b) {
+          const int c = (2 * b + half) * 32 + lane;
+          bv[b] = bias && c < nv ? __ldg(bias + c_tile + c) : 0.f;
+        }
         for (int ch = 0; ch < chunks && ok; ++ch) {
           if (!tc::mbar_wait(&acc_full[as], aph, abort_flag)) { ok = false; break; }
           tc::tc_fence_after();
@@ -299,10 +313,16 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
           if (++as == 2) { as = 0; aph ^= 1u; }
         }
         if (!ok) break;
+        if (bias) {
+          __syncwarp();  // the last tile's have been read
+#pragma unroll
+          for (int b = 0; b < kHtBlocks; ++b) my_bias[b * 32 + lane] = bv[b];
+          __syncwarp();
+        }
 #pragma unroll
         for (int b = 0; b < kHtBlocks; ++b) {
           const int c = (2 * b + half) * 32;
-          if (c < nv) ht_block_stats(l[b], st, c_tile + c, nv - c, bias, y, a.at_label + i);
+          if (c < nv) ht_block_stats(l[b], st, c_tile + c, nv - c, bias ? my_bias + b * 32 : nullptr, y, a.at_label + i);
         }
       }
       if (!ok) {
