@@ -48,7 +48,7 @@ struct Layout {
   bool vec4 = true;
   // byte offsets into the workspace
   size_t x, v, g, g1b, g1keep, xpkeep, xop, acc, yring, gprev, tmp, idx, ylab, sched, partial, scalars, status, gbar1, gbar2;
-  size_t act[9], mask[9], logits, rowloss, dz[2], dh[2], xstage, ystage, xstage2, ystage2;
+  size_t act[9], mask[9], logits, rowloss, dz[2], dh[2], xstage, ystage, xstage2, ystage2, xcall;
   // fp32 GEMMs on the bf16 tensor cores (LSAM_GEMM_FP32 with LSAM_IMPL_TCGEN05): the parameters the next gradient pass reads,
   // activations and backward signals are stored as three bf16 planes each; xpl = planes of the parameters [3][K][ld]
   bool x3 = false;
@@ -179,7 +179,7 @@ bool plan(const lsam_config& c, Layout& L) {
   L.partial = take(4 * K * (size_t)L.nchunks);
   L.ylab = take(4 * K * B);
   for (int i = 0; i < 9; ++i) L.act[i] = L.mask[i] = 0;
-  L.logits = L.rowloss = L.dz[0] = L.dz[1] = L.dh[0] = L.dh[1] = L.xstage = L.ystage = L.xstage2 = L.ystage2 = 0;
+  L.logits = L.rowloss = L.dz[0] = L.dz[1] = L.dh[0] = L.dh[1] = L.xstage = L.ystage = L.xstage2 = L.ystage2 = L.xcall = 0;
   for (int i = 0; i < 9; ++i) L.col[i] = L.parg[i] = 0;
   L.zout = L.dzc = L.dcol = L.wpart = 0;
   if (!flat) {
@@ -192,6 +192,9 @@ bool plan(const lsam_config& c, Layout& L) {
     L.xstage2 = take(4 * K * B * in0);  // second slot of the prefetch queue (lsam_stage_batch)
     L.ystage2 = take(4 * K * B);
     if (c.model != LSAM_MODEL_LSQ) {
+      // the minibatch of lsam_step_batch and lsam_score_batch, written and read on the context's stream alone: the prefetch queue's slots are
+      // written on its copy stream, at any time
+      L.xcall = take(4 * K * B * in0);
       size_t maxw = 0, max_full = 0, max_dcol = 0, max_part = 0;
       for (size_t l = 0; l < L.layers.size(); ++l) {
         LayerInfo& li = L.layers[l];
@@ -1300,7 +1303,7 @@ int lsam_step_batch(lsam_ctx* c, float eta, float rho, const float* xb, const vo
   const int64_t nx = rows * c->L.in0;
   const cudaMemcpyKind kind = on_host ? cudaMemcpyHostToDevice : cudaMemcpyDeviceToDevice;
   const bool lsq = cfg.model == LSAM_MODEL_LSQ;
-  float* xdst = lsq ? c->at<float>(c->L.act[0]) : c->at<float>(c->L.xstage);  // classifiers: staged, then stored feature-major
+  float* xdst = lsq ? c->at<float>(c->L.act[0]) : c->at<float>(c->L.xcall);  // classifiers: then stored feature-major
   c->launches += 2;
   LSAM_CUDA(c, cudaMemcpyAsync(xdst, xb, sizeof(float) * nx, kind, c->stream));
   LSAM_CUDA(c, cudaMemcpyAsync(c->at<uint32_t>(c->L.ylab), yb, 4 * rows, kind, c->stream));
@@ -1328,12 +1331,12 @@ int lsam_score_batch(lsam_ctx* c, const float* xb, const int32_t* yb, int on_hos
   if (cfg.model == LSAM_MODEL_FLAT || cfg.model == LSAM_MODEL_LSQ) return c->fail(LSAM_ERR_INVALID, "lsam_score_batch: classifiers only");
   if (d_logp && !yb) return c->fail(LSAM_ERR_INVALID, "lsam_score_batch: d_logp without labels");
   if (top_k < 0 || top_k > LSAM_TOP_MAX || (top_k > 0 && (!d_top_logp || !d_top_idx))) return c->fail(LSAM_ERR_INVALID, "lsam_score_batch: top_k outside 0 .. LSAM_TOP_MAX, or its arrays missing");
-  if (c->stage_count > 0) return c->fail(LSAM_ERR_STATE, "lsam_score_batch: a staged minibatch is waiting in the buffers this call would use");
+  if (c->stage_count > 0) return c->fail(LSAM_ERR_STATE, "lsam_score_batch: a staged minibatch is waiting (lsam_step_staged takes it)");
   if (int rc = c->check_device()) return rc;
   const int K = cfg.K, B = cfg.batch;
   const int64_t rows = (int64_t)K * B;
   const cudaMemcpyKind kind = on_host ? cudaMemcpyHostToDevice : cudaMemcpyDeviceToDevice;
-  float* xdst = c->at<float>(L.xstage);
+  float* xdst = c->at<float>(L.xcall);
   c->launches += 1;
   LSAM_CUDA(c, cudaMemcpyAsync(xdst, xb, sizeof(float) * rows * L.in0, kind, c->stream));
   if (yb) {
