@@ -1379,6 +1379,9 @@ int lsam_stage_batch(lsam_ctx* c, const float* xb, const void* yb, int on_host) 
       LSAM_CUDA(c, cudaEventCreateWithFlags(&c->staged_done[i], cudaEventDisableTiming));
       LSAM_CUDA(c, cudaEventCreateWithFlags(&c->slot_free[i], cudaEventDisableTiming));
     }
+    // lsam_init clears the workspace on the context's stream: the first copies come behind that
+    LSAM_CUDA(c, cudaEventRecord(c->slot_free[0], c->stream));
+    LSAM_CUDA(c, cudaStreamWaitEvent(c->copy_stream, c->slot_free[0], 0));
   }
   const int slot = (c->stage_head + c->stage_count) & 1;
   const int64_t rows = (int64_t)cfg.K * cfg.batch;

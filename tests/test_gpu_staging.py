@@ -79,3 +79,35 @@ def test_a_supplied_minibatch_beside_staged_ones(name, on_device):
         for i in (1, 3, 0, 2, 0, 3):
             b.step_batch(0.02, 0.05, *x[i])
     same(a, b)
+
+
+class Unsynchronised(torch.cuda.Stream):
+    """A stream on which the binding's wait after lsam_init does nothing, as for a caller of the C interface that does not wait."""
+
+    def synchronize(self):
+        pass
+
+
+def test_a_minibatch_staged_right_after_init_is_not_cleared_with_the_workspace():
+    rng = np.random.default_rng(0)
+    cfg = G.make_config(G.MODEL_MLP, widths=(40, 64, 10), K=2, batch=16, n_samples=64, tau=64, lam=0.1, seed=3)
+    d = G.lsam_param_count(cfg)
+    x0 = torch.from_numpy((rng.standard_normal((2, d)) * 0.08).astype(np.float32)).cuda()
+    X, Y, y0 = torch.zeros((64, 40), device="cuda"), torch.zeros(64, device="cuda", dtype=torch.int32), x0.mean(0)
+    xb, yb = torch.randn((2, 16, 40), device="cuda"), torch.randint(0, 10, (2, 16), device="cuda", dtype=torch.int32)
+    runs = []
+    for _ in range(2):
+        stream = Unsynchronised()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(int(20 * 1.9e6))
+        ctx = G.Lsam(cfg, X, Y, x0, y0, stream=stream)
+        if runs:
+            torch.cuda.synchronize()
+        ctx.stage_batch(xb, yb)
+        ctx.step_staged(0.02, 0.05)
+        torch.cuda.synchronize()
+        runs.append((ctx, ctx.read_all_params()))
+    assert np.array_equal(runs[0][1], runs[1][1])
+    for ctx, _ in runs:
+        ctx.close()
