@@ -289,7 +289,7 @@ int64_t lsam_launch_count(const lsam_ctx* ctx);
 /* 1 if the model GEMMs of this context run on the tcgen05 tensor-core path, 0 if on the SIMT path. */
 int lsam_uses_tcgen05(const lsam_ctx* ctx);
 const char* lsam_last_error(const lsam_ctx* ctx);
-/* Frees the host context only; the caller frees the workspace. */
+/* Frees the host context only; the caller frees the workspace, once the context's stream has finished (copies of staged minibatches have, on return). */
 void lsam_destroy(lsam_ctx* ctx);
 
 /* Host-side statement of the schedule hash, H(seed, tag, t, k, j) = mix(mix(mix(seed ^ tag) + t) + (k 2^20 + j))

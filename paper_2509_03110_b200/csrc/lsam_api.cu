@@ -1779,7 +1779,10 @@ void lsam_destroy(lsam_ctx* c) {
     if (c->staged_done[i]) cudaEventDestroy(c->staged_done[i]);
     if (c->slot_free[i]) cudaEventDestroy(c->slot_free[i]);
   }
-  if (c->copy_stream) cudaStreamDestroy(c->copy_stream);
+  if (c->copy_stream) {
+    cudaStreamSynchronize(c->copy_stream);  // a minibatch that was staged and never stepped: the caller frees the workspace next
+    cudaStreamDestroy(c->copy_stream);
+  }
   delete c;
 }
 

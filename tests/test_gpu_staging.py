@@ -111,3 +111,19 @@ def test_a_minibatch_staged_right_after_init_is_not_cleared_with_the_workspace()
     assert np.array_equal(runs[0][1], runs[1][1])
     for ctx, _ in runs:
         ctx.close()
+
+
+def test_a_staged_copy_has_ended_when_the_context_has():
+    K, B, n = 16, 512, 4096  # 134 MB: a few milliseconds from pinned memory
+    cfg = G.make_config(G.MODEL_LSQ, widths=(n,), K=K, batch=B, n_samples=64, tau=64, lam=0.1, seed=3)
+    x0 = torch.zeros((K, G.lsam_param_count(cfg)), device="cuda")
+    ctx = G.Lsam(cfg, torch.zeros((64, n), device="cuda"), torch.zeros(64, device="cuda"), x0, x0[0].clone())
+    xb, yb = torch.full((K, B, n), 3.0).pin_memory(), torch.zeros((K, B)).pin_memory()
+    at, nbytes = ctx.workspace.data_ptr(), ctx.workspace.numel()
+    ctx.stage_batch(xb, yb)
+    ctx.close()
+    del ctx
+    z = torch.full((nbytes,), 7, dtype=torch.uint8, device="cuda")
+    assert z.data_ptr() == at  # the workspace's memory
+    torch.cuda.synchronize()
+    assert (z == 7).all()
