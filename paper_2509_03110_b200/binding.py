@@ -258,10 +258,15 @@ def _ptr(t, what, shape, dtype, dev):
     return t.data_ptr()
 
 
-def _on(stream, fn):
-    """Runs an operator with `stream` as the current stream, so that what it allocates belongs to that stream."""
+def _on(stream, fn, *tensors):
+    """Runs an operator with `stream` as the current stream, so that what it allocates belongs to that stream.  The memory of `tensors`, what the
+    caller handed in, is not handed out again before `stream` has passed the call, even if the caller drops them at once."""
     with _torch.cuda.stream(stream):
-        return fn()
+        r = fn()
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return r
 
 
 def lsam_logprob(logits, labels=None, top_k=0, stream=None):
@@ -269,11 +274,13 @@ def lsam_logprob(logits, labels=None, top_k=0, stream=None):
 
     logits: [rows, classes] or [K, rows, classes], float32 / bfloat16 / float16, any strides (a context's own logits have the sample
     index contiguous: a transposed view).  labels: int32 [rows] / [K, rows]; negative = the row is left out (zeros, index -1), None = no
-    logp.  The rules for masks, NaN and ties stand in include/lsam.h.  Returns LogProb.  stream: None = the current one.
+    logp.  The rules for masks, NaN and ties stand in include/lsam.h.  Returns LogProb.
+    stream: None = the current one.  Another one has to be ordered behind what produced the inputs; the results belong to it, so a stream that reads
+    them has to be ordered behind it in turn.  (The same for the other operators.)
     """
     torch = _load()
     if stream is not None:
-        return _on(stream, lambda: lsam_logprob(logits, labels, top_k))
+        return _on(stream, lambda: lsam_logprob(logits, labels, top_k), logits, labels)
     K, R, V, sk, sr, sc = _stacked(logits, "logits")
     code = _code(logits, "logits")
     dev = logits.device
@@ -305,7 +312,7 @@ def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, o
     """
     torch = _load()
     if stream is not None:
-        return _on(stream, lambda: lsam_logprob_grad(logits, labels, lse, dlogp, entropy, dentropy, out))
+        return _on(stream, lambda: lsam_logprob_grad(logits, labels, lse, dlogp, entropy, dentropy, out), logits, labels, lse, dlogp, entropy, dentropy, out)
     K, R, V, sk, sr, sc = _stacked(logits, "logits")
     code = _code(logits, "logits")
     dev = logits.device
@@ -333,7 +340,7 @@ def lsam_head_logprob(h, w, labels=None, bias=None, stream=None):
     """
     torch = _load()
     if stream is not None:
-        return _on(stream, lambda: lsam_head_logprob(h, w, labels, bias))
+        return _on(stream, lambda: lsam_head_logprob(h, w, labels, bias), h, w, labels, bias)
     K, R, D, hk, hr, hc = _stacked(h, "h")
     KW, V, DW, wk, wc, wi = _stacked(w, "w")
     code = _code(h, "h")
@@ -373,7 +380,7 @@ def lsam_dropout(x, p, seed, tick, layer=0, k_offset=0, skip=None, out=None, str
     """
     torch = _load()
     if stream is not None:
-        return _on(stream, lambda: lsam_dropout(x, p, seed, tick, layer, k_offset, skip, out))
+        return _on(stream, lambda: lsam_dropout(x, p, seed, tick, layer, k_offset, skip, out), x, skip, out)
     K, R, n, xk, xr, xc = _stacked(x, "x")
     code = _code(x, "x")
     dev = x.device
@@ -481,7 +488,8 @@ class Lsam:
     def score_batch(self, xb, yb=None, top_k=0):
         """Log probability of the labels, log-sum-exp, entropy and top_k alternatives of a minibatch under every worker's iterate.
 
-        xb [K, B, in] float32, yb [K, B] int32 or None: both CUDA tensors, or both host tensors / numpy arrays.  Returns LogProb of CUDA tensors [K, B].
+        xb [K, B, in] float32, yb [K, B] int32 or None: both CUDA tensors, or both host tensors / numpy arrays (pinned ones are read when the context's
+        stream gets there: they must stay as they are, and be kept, until it has passed the call).  Returns LogProb of CUDA tensors [K, B].
         Runs on the context's stream: other streams order their reads of the result behind it, and it behind what produced xb and yb.
         """
         torch = _load()
