@@ -348,6 +348,12 @@ int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, i
                  int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
                  float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len);
 
+/* The same with log-sum-exp in two words: d_lse_low (nullable) receives what the rounding of lse to 32 bits leaves out, so that lse + lse_low keeps the
+ * digits of log sum e^(l - max l) however large the logits are (0 in rows that are left out or hold nothing but masks). */
+int lsam_logprob_wide(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                      int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_lse_low, float* d_entropy,
+                      float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len);
+
 /* Gradient of a loss of logp and entropy with respect to the logits:
  *   dlogits[c] = dlogp (1[c = label] - p_c) - dentropy p_c (log p_c + entropy),   p_c = e^(l[c] - lse)
  * with lse and entropy [K, rows] as lsam_logprob returned them for the same logits, dlogp and dentropy [K, rows] the loss's derivatives
@@ -359,6 +365,14 @@ int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t ro
                       int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
                       const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
                       void* cuda_stream, char* h_err, size_t h_err_len);
+
+/* The same with both words of lsam_logprob_wide: p_c = e^(l[c] - lse - lse_low).  With lse alone every p_c of a row is off by a factor of
+ * 1 +- |lse| 2^-24: nothing to speak of for usual logits, 1.6e-4 in fp32 rows around 1e4 (whose logits are themselves that far apart), and no
+ * distribution any more where all logits are large, such as a row that an additive mask of -1e9 has emptied.  d_lse_low: nullable (0). */
+int lsam_logprob_grad_wide(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                           int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_lse_low, const float* d_entropy,
+                           const float* d_dlogp, const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row,
+                           int64_t out_stride_class, void* cuda_stream, char* h_err, size_t h_err_len);
 
 /* The first three results of lsam_logprob for the logits l = h w^T + bias, which are never stored:
  *  d_h [K, rows, inner] and d_w [K, classes, inner] of `dtype`, the inner index contiguous; w_stride_k = 0 shares one head among the workers.

@@ -29,7 +29,7 @@ EXPORTS = [
     "lsam_profile_enable", "lsam_profile_read", "lsam_launch_count", "lsam_uses_tcgen05", "lsam_last_error",
     "lsam_destroy", "lsam_schedule_hash", "lsam_row_norms_static", "lsam_acc_buffer", "lsam_selftest_bounded_wait",
     "lsam_checkpoint_bytes", "lsam_save_checkpoint", "lsam_load_checkpoint", "lsam_read_anchor_gap",
-    "lsam_logprob", "lsam_logprob_grad", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout", "lsam_score_batch",
+    "lsam_logprob", "lsam_logprob_grad", "lsam_logprob_wide", "lsam_logprob_grad_wide", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout", "lsam_score_batch",
 ]
 
 
@@ -113,6 +113,8 @@ def lib():
     i32, i64, err = C.c_int32, C.c_int64, [vp, C.c_char_p, C.c_size_t]  # err: stream and error buffer
     L.lsam_logprob.argtypes = [vp, i32, i32] + [i64] * 5 + [vp, i32] + [vp] * 5 + err
     L.lsam_logprob_grad.argtypes = [vp, i32, i32] + [i64] * 5 + [vp] * 6 + [i64] * 3 + err
+    L.lsam_logprob_wide.argtypes = [vp, i32, i32] + [i64] * 5 + [vp, i32] + [vp] * 6 + err
+    L.lsam_logprob_grad_wide.argtypes = [vp, i32, i32] + [i64] * 5 + [vp] * 7 + [i64] * 3 + err
     L.lsam_head_logprob_workspace_bytes.restype = C.c_size_t
     L.lsam_head_logprob_workspace_bytes.argtypes = [i32, i32, i64, i64, i64, i32]
     L.lsam_head_logprob.argtypes = [vp, vp, vp, i32, i32] + [i64] * 8 + [vp] * 5 + [C.c_size_t] + err
@@ -176,14 +178,20 @@ HEAD_ALIGNED, HEAD_SHARED = 1, 2
 TOP_MAX, DROPOUT_LAYERS, DROPOUT_WORKERS = 32, 4096, 1 << 20
 
 
-class LogProb(NamedTuple):
-    """Scores of rows of logits: fp32 [..., rows] (top_logp and int32 top_idx: [..., rows, top_k]); None where not asked for."""
-
+class _Scores(NamedTuple):
     logp: object
     lse: object
     entropy: object
     top_logp: object
     top_idx: object
+
+
+class LogProb(_Scores):
+    """Scores of rows of logits: fp32 [..., rows] (top_logp and int32 top_idx: [..., rows, top_k]); None where not asked for.
+
+    lse_low, beside the tuple: what the rounding of lse to 32 bits leaves out (lsam_logprob only, else None)."""
+
+    lse_low = None
 
 
 def _invalid(msg):
@@ -284,35 +292,49 @@ def lsam_logprob(logits, labels=None, top_k=0, stream=None):
     K, R, V, sk, sr, sc = _stacked(logits, "logits")
     code = _code(logits, "logits")
     dev = logits.device
-    lead = logits.shape[:-1]
+    lead = (K, R) if logits.dim() == 3 else (R,)
     pl = None if labels is None else _ptr(labels, "labels", lead, torch.int32, dev)
-    f32 = _proto(dev)
+    n = 4 * K * R  # bytes of a per-row result
+    buf = _proto(dev).new_empty((3 if labels is None else 4, *lead))
     if labels is None:
-        logp = None
-        lse, ent = f32.new_empty((2, *lead)).unbind(0)
+        logp = pp = None
+        lse, ent, low = buf.unbind(0)
+        p = buf.data_ptr()
     else:
-        logp, lse, ent = f32.new_empty((3, *lead)).unbind(0)
+        logp, lse, ent, low = buf.unbind(0)
+        pp = buf.data_ptr()
+        p = pp + n
     tv = ti = pv = pi = None
     if top_k:
         if not 0 < top_k <= TOP_MAX:
             raise _invalid(f"top_k outside 0 .. {TOP_MAX}")
-        tv, ti = f32.new_empty((2, *lead, top_k)).unbind(0)
+        buf = buf.new_empty((2, *lead, top_k))
+        tv, ti = buf.unbind(0)
         ti = ti.view(torch.int32)
-        pv, pi = tv.data_ptr(), ti.data_ptr()
-    _call(lib().lsam_logprob, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, top_k, None if logp is None else logp.data_ptr(), lse.data_ptr(), ent.data_ptr(), pv, pi,
-          _raw_stream(dev))
-    return LogProb(logp, lse, ent, tv, ti)
+        pv = buf.data_ptr()
+        pi = pv + n * top_k
+    _call(lib().lsam_logprob_wide, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, top_k, pp, p, p + 2 * n, p + n, pv, pi, _raw_stream(dev))
+    r = tuple.__new__(LogProb, (logp, lse, ent, tv, ti))  # without the check of a named tuple's arguments
+    r.lse_low = low
+    return r
 
 
-def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, out=None, stream=None):
+def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, out=None, stream=None, lse_low=None):
     """Gradient with respect to the logits of a loss whose derivatives by logp and entropy are dlogp and dentropy (either may be None).
 
-    lse and entropy: what lsam_logprob returned for these logits.  out: tensor of the logits' shape and type to write (logits itself is
+    lse: what lsam_logprob returned for these logits, whole (then entropy and lse_low are taken from it where they are not given), or its lse alone, with
+    which the probabilities of a row are off by a factor of 1 +- |lse| 2^-24.  out: tensor of the logits' shape and type to write (logits itself is
     allowed), None = a new one.  Returns it.
     """
     torch = _load()
+    if isinstance(lse, LogProb):
+        if lse_low is None:
+            lse_low = lse.lse_low
+        if entropy is None and dentropy is not None:
+            entropy = lse.entropy
+        lse = lse.lse
     if stream is not None:
-        return _on(stream, lambda: lsam_logprob_grad(logits, labels, lse, dlogp, entropy, dentropy, out), logits, labels, lse, dlogp, entropy, dentropy, out)
+        return _on(stream, lambda: lsam_logprob_grad(logits, labels, lse, dlogp, entropy, dentropy, out, None, lse_low), logits, labels, lse, dlogp, entropy, dentropy, out, lse_low)
     K, R, V, sk, sr, sc = _stacked(logits, "logits")
     code = _code(logits, "logits")
     dev = logits.device
@@ -322,13 +344,13 @@ def lsam_logprob_grad(logits, labels, lse, dlogp, entropy=None, dentropy=None, o
     ps = _ptr(lse, "lse", lead, f32, dev)
     if ps is None:
         raise _invalid("lse is needed")
-    pe, pa, pb = _ptr(entropy, "entropy", lead, f32, dev), _ptr(dlogp, "dlogp", lead, f32, dev), _ptr(dentropy, "dentropy", lead, f32, dev)
+    pw, pe, pa, pb = _ptr(lse_low, "lse_low", lead, f32, dev), _ptr(entropy, "entropy", lead, f32, dev), _ptr(dlogp, "dlogp", lead, f32, dev), _ptr(dentropy, "dentropy", lead, f32, dev)
     if out is None:
         out = torch.empty_like(logits)
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
         raise _invalid("out must have the shape, type and device of logits")
     ok, orow, oc = _stacked(out, "out")[3:]
-    _call(lib().lsam_logprob_grad, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, ps, pe, pa, pb, out.data_ptr(), ok, orow, oc, _raw_stream(dev))
+    _call(lib().lsam_logprob_grad_wide, logits.data_ptr(), code, K, R, V, sk, sr, sc, pl, ps, pw, pe, pa, pb, out.data_ptr(), ok, orow, oc, _raw_stream(dev))
     return out
 
 

@@ -78,6 +78,11 @@ __device__ inline RowScore stat_finish(const RowStat& a) {
   const float b = log2f(a.s), ls = b / kLog2e;
   return {a.m, ls, a.m + ls, (b - a.t / a.s) / kLog2e};
 }
+// lse + lse_low(r) is m + ls to twice the digits (the error of the sum m + ls, exact in six additions)
+__device__ inline float lse_low(const RowScore& r) {
+  const float s = r.m + r.ls, b = s - r.m;
+  return (r.m - (s - b)) + (r.ls - b);
+}
 __device__ inline float score_logp(float l, const RowScore& r) { return l <= kMasked ? -INFINITY : (l - r.m) - r.ls; }
 
 // Order of the alternatives: larger logit first, then the lower class.  One 64-bit key per element (0: not an alternative,
@@ -108,6 +113,7 @@ struct ScoreOut {
   float *logp, *lse, *entropy, *top_logp;  // each nullable
   int32_t* top_idx;
   int32_t top_k;
+  float* lse_low;  // nullable: what the rounding of lse to 32 bits leaves out
 };
 
 // What a row that is left out (negative label) or has no finite logit returns beside its statistics.
@@ -476,12 +482,14 @@ __device__ inline void write_left_out(const ScoreOut& o, int64_t i) {
   if (o.logp) o.logp[i] = 0.f;
   if (o.lse) o.lse[i] = 0.f;
   if (o.entropy) o.entropy[i] = 0.f;
+  if (o.lse_low) o.lse_low[i] = 0.f;
   write_no_top(o, i, 0);
 }
 __device__ inline void write_scores(const ScoreOut& o, int64_t i, const RowScore& sc, int32_t y, int32_t classes, float at_label) {
   if (o.logp) o.logp[i] = y < classes ? score_logp(at_label, sc) : NAN;
   if (o.lse) o.lse[i] = sc.lse;
   if (o.entropy) o.entropy[i] = sc.ent;
+  if (o.lse_low) o.lse_low[i] = lse_low(sc);
 }
 __device__ inline void write_top(const ScoreOut& o, int64_t i, int j, uint64_t key, const RowScore& sc) {
   o.top_logp[i * o.top_k + j] = key ? score_logp(order_value((uint32_t)(key >> 32)), sc) : -INFINITY;
@@ -830,13 +838,17 @@ logprob_thread_kernel(LogitView<T> v, const int32_t* __restrict__ labels, ScoreO
 // a = dL/dlogp, b = dL/dH (each nullable = 0).  Rows that are left out (y < 0) or hold nothing but masks (lse = -inf) get 0.
 // With u = l - lse it is p (c0 + c1 u), c0 = -(a + b H), c1 = -b, plus a at the label: one read, one write, two multiply-adds and one exponential
 // per element, bound by the bytes.
+// lse rounded to 32 bits is off by up to |lse| 2^-24, and every p of the row with it.  With its low word d, p = e^(u - d), u = l - lse, and
+// p (c0 + c1 (u - d)) = e^u (c0' + c1' u) with c1' = c1 e^-d, c0' = (c0 - c1 d) e^-d: the row's coefficients take it, an element costs nothing more.
+// TWO: with the low word.  Compiled apart, because a row's threads repeat its coefficients (2048 x 131072 bf16: 171 us, 177 with a test of the pointer there).
 struct GradIn {
   const int32_t* labels;
-  const float *lse, *entropy, *dlogp, *dentropy;
+  const float *lse, *entropy, *dlogp, *dentropy, *lse_low;
 };
 template <typename T>
 struct GradOut { T* p; int64_t sk, sr, sc; };
 
+template <bool TWO>
 struct GradRow {
   float lse, c0, c1, at_label;
   int32_t y;   // class that receives at_label, -1: none, -2: the whole row is zero
@@ -849,6 +861,11 @@ struct GradRow {
     c0 = -a - (g.dentropy ? b * g.entropy[i] : 0.f);
     c1 = -b;
     at_label = a;
+    if constexpr (TWO) {
+      const float d = g.lse_low[i], f = expf(-d);
+      c0 = f * fmaf(-c1, d, c0);
+      c1 *= f;
+    }
     if ((g.labels && y < 0) || lse == -INFINITY) y = -2;
     if (y >= classes) c0 = NAN;  // the whole row
   }
@@ -873,7 +890,7 @@ template <typename T> __device__ inline uint4 vec_pack(const float (&f)[16 / siz
 // same 16-byte phase (the host checks the strides), so that both move as vectors; UNIT: contiguous, consecutive lanes move consecutive elements; ANY: any stride.
 enum : int { GRAD_VECTORS = 0, GRAD_UNIT = 1, GRAD_ANY = 2 };
 template <typename T> __host__ __device__ constexpr int64_t grad_chunk(int mode, int NT) { return mode == GRAD_VECTORS ? (int64_t)NT * 4 * vec_n<T>() : (int64_t)NT * 8; }
-template <typename T, int NT, int MODE>
+template <typename T, int NT, int MODE, bool TWO>
 __global__ void __launch_bounds__(256)
 grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, FastDiv by_chunks, uint32_t units) {
   constexpr int N = vec_n<T>();
@@ -893,7 +910,7 @@ grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, FastDiv by_chunks, uin
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (q0 + e * NT < rp.nvec) x[e] = from[e * NT];
-    const GradRow row(g, i, v.classes);
+    const GradRow<TWO> row(g, i, v.classes);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (q0 + e * NT >= rp.nvec) break;
@@ -919,7 +936,7 @@ grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, FastDiv by_chunks, uin
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e < n) x[e] = from[e * NT * si];
-    const GradRow row(g, i, v.classes);
+    const GradRow<TWO> row(g, i, v.classes);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e < n) to[e * NT * so] = from_float<T>(row(to_float(x[e]), (int32_t)c0 + e * NT));
@@ -928,7 +945,7 @@ grad_row_kernel(LogitView<T> v, GradIn g, GradOut<T> out, FastDiv by_chunks, uin
 
 // Logits and gradient with the sample index contiguous: a thread owns R consecutive rows (a 16-byte vector, or one row where the strides do
 // not allow it) and 8 classes of a block's 64.  block (32, 8), grid K * row blocks * class blocks.
-template <typename T, int R>
+template <typename T, int R, bool TWO>
 __global__ void __launch_bounds__(256, R == 8 ? 3 : R == 1 ? 5 : 4)
 grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_blocks, uint32_t class_blocks) {
   const uint32_t cb = blockIdx.x % class_blocks, kr = blockIdx.x / class_blocks, rb = kr % row_blocks, k = kr / row_blocks;
@@ -936,10 +953,10 @@ grad_feature_kernel(LogitView<T> v, GradIn g, GradOut<T> out, uint32_t row_block
   if (r0 >= v.rows) return;
   const T* src = v.p + k * v.sk + r0;
   T* dst = out.p + k * out.sk + r0;
-  GradRow row[R];
+  GradRow<TWO> row[R];
 #pragma unroll
   for (int j = 0; j < R; ++j)
-    if (r0 + j < v.rows) row[j] = GradRow(g, (int64_t)k * v.rows + r0 + j, v.classes);
+    if (r0 + j < v.rows) row[j] = GradRow<TWO>(g, (int64_t)k * v.rows + r0 + j, v.classes);
   const int64_t c0 = (int64_t)cb * 64 + threadIdx.y;
   if (R > 1 && r0 + R <= v.rows) {
     constexpr int N = vec_n<T>();

@@ -143,10 +143,10 @@ cudaError_t launch_scores(const LogitView<T>& v, const int32_t* labels, const Sc
 
 }  // namespace
 
-extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
-                            int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
-                            float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len) {
-  const Err err("lsam_logprob", h_err, h_err_len);
+namespace {
+
+int logprob(const Err& err, const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row, int64_t stride_class,
+            const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_lse_low, float* d_entropy, float* d_top_logp, int32_t* d_top_idx, void* cuda_stream) {
   if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
   if (K < 0 || rows < 0 || classes < 1 || classes > kMaxIndex) return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= classes < 2^31");
   if (top_k < 0 || top_k > LSAM_TOP_MAX) return err.fail(LSAM_ERR_INVALID, "top_k outside 0 .. LSAM_TOP_MAX");
@@ -156,10 +156,10 @@ extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int6
   if (!strides_ok(K, stride_k, rows, stride_row, classes, stride_class)) return err.fail(LSAM_ERR_INVALID, "a stride is negative or the tensor is too large");
   PtrCheck pc;
   pc.need(d_logits, dtype_size(dtype));
-  pc.optional(d_labels, 4); pc.optional(d_logp, 4); pc.optional(d_lse, 4); pc.optional(d_entropy, 4);
+  pc.optional(d_labels, 4); pc.optional(d_logp, 4); pc.optional(d_lse, 4); pc.optional(d_entropy, 4); pc.optional(d_lse_low, 4);
   if (top_k > 0) { pc.need(d_top_logp, 4); pc.need(d_top_idx, 4); }
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
-  const ScoreOut out{d_logp, d_lse, d_entropy, d_top_logp, d_top_idx, top_k};
+  const ScoreOut out{d_logp, d_lse, d_entropy, d_top_logp, d_top_idx, top_k, d_lse_low};
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
@@ -170,11 +170,27 @@ extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int6
   return err.done(e);
 }
 
+}  // namespace
+
+extern "C" int lsam_logprob(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                            int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_entropy,
+                            float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len) {
+  return logprob(Err("lsam_logprob", h_err, h_err_len), d_logits, dtype, K, rows, classes, stride_k, stride_row, stride_class, d_labels, top_k, d_logp, d_lse, nullptr,
+                 d_entropy, d_top_logp, d_top_idx, cuda_stream);
+}
+
+extern "C" int lsam_logprob_wide(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                                 int64_t stride_class, const int32_t* d_labels, int32_t top_k, float* d_logp, float* d_lse, float* d_lse_low, float* d_entropy,
+                                 float* d_top_logp, int32_t* d_top_idx, void* cuda_stream, char* h_err, size_t h_err_len) {
+  return logprob(Err("lsam_logprob_wide", h_err, h_err_len), d_logits, dtype, K, rows, classes, stride_k, stride_row, stride_class, d_labels, top_k, d_logp, d_lse, d_lse_low,
+                 d_entropy, d_top_logp, d_top_idx, cuda_stream);
+}
+
 namespace {
 
 // Form of a gradient call: vectors along the classes or along the samples where both tensors have that index contiguous and every row of
 // the two starts at the same place of a 16-byte vector, single elements in the same order otherwise.
-template <typename T>
+template <typename T, bool TWO>
 cudaError_t launch_grad(const LogitView<T>& v, const GradIn& in, const GradOut<T>& o, int32_t K, cudaStream_t stream) {
   const int64_t total = (int64_t)K * v.rows;
   const auto aligned = [](int64_t elems) { return elems * (int64_t)sizeof(T) % 16 == 0; };
@@ -184,8 +200,8 @@ cudaError_t launch_grad(const LogitView<T>& v, const GradIn& in, const GradOut<T
     const int64_t class_blocks = ceil_div(v.classes, 64), row_blocks = ceil_div(v.rows, vec ? 32 * vec_n<T>() : 32);
     if (class_blocks * row_blocks <= kMaxIndex / K) {
       const unsigned grid = (unsigned)(class_blocks * row_blocks * K);
-      if (vec) grad_feature_kernel<T, vec_n<T>()><<<grid, dim3(32, 8), 0, stream>>>(v, in, o, (uint32_t)row_blocks, (uint32_t)class_blocks);
-      else grad_feature_kernel<T, 1><<<grid, dim3(32, 8), 0, stream>>>(v, in, o, (uint32_t)row_blocks, (uint32_t)class_blocks);
+      if (vec) grad_feature_kernel<T, vec_n<T>(), TWO><<<grid, dim3(32, 8), 0, stream>>>(v, in, o, (uint32_t)row_blocks, (uint32_t)class_blocks);
+      else grad_feature_kernel<T, 1, TWO><<<grid, dim3(32, 8), 0, stream>>>(v, in, o, (uint32_t)row_blocks, (uint32_t)class_blocks);
       return cudaPeekAtLastError();
     }
   }
@@ -199,7 +215,7 @@ cudaError_t launch_grad(const LogitView<T>& v, const GradIn& in, const GradOut<T
   };
   const auto pick = [&](auto mode) {
     constexpr int M = decltype(mode)::value;
-    return narrow ? go(grad_row_kernel<T, 32, M>, grad_chunk<T>(M, 32)) : go(grad_row_kernel<T, 256, M>, grad_chunk<T>(M, 256));
+    return narrow ? go(grad_row_kernel<T, 32, M, TWO>, grad_chunk<T>(M, 32)) : go(grad_row_kernel<T, 256, M, TWO>, grad_chunk<T>(M, 256));
   };
   if (vec) return pick(std::integral_constant<int, GRAD_VECTORS>());
   return unit ? pick(std::integral_constant<int, GRAD_UNIT>()) : pick(std::integral_constant<int, GRAD_ANY>());
@@ -207,11 +223,11 @@ cudaError_t launch_grad(const LogitView<T>& v, const GradIn& in, const GradOut<T
 
 }  // namespace
 
-extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
-                                 int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
-                                 const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
-                                 void* cuda_stream, char* h_err, size_t h_err_len) {
-  const Err err("lsam_logprob_grad", h_err, h_err_len);
+namespace {
+
+int logprob_grad(const Err& err, const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row, int64_t stride_class,
+                 const int32_t* d_labels, const float* d_lse, const float* d_lse_low, const float* d_entropy, const float* d_dlogp, const float* d_dentropy, void* d_dlogits,
+                 int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class, void* cuda_stream) {
   if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
   if (K < 0 || rows < 0 || classes < 1 || classes > kMaxIndex) return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= classes < 2^31");
   if (!d_dlogp && !d_dentropy) return err.fail(LSAM_ERR_INVALID, "neither d_dlogp nor d_dentropy is given");
@@ -224,18 +240,36 @@ extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K,
   if (!disjoint(K, out_stride_k, rows, out_stride_row, classes, out_stride_class)) return err.fail(LSAM_ERR_INVALID, "elements of the gradient share an address or interleave");
   PtrCheck pc;
   pc.need(d_logits, dtype_size(dtype)); pc.need(d_dlogits, dtype_size(dtype)); pc.need(d_lse, 4);
-  pc.optional(d_labels, 4); pc.optional(d_entropy, 4); pc.optional(d_dlogp, 4); pc.optional(d_dentropy, 4);
+  pc.optional(d_labels, 4); pc.optional(d_entropy, 4); pc.optional(d_dlogp, 4); pc.optional(d_dentropy, 4); pc.optional(d_lse_low, 4);
   if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
-  const GradIn in{d_labels, d_lse, d_entropy, d_dlogp, d_dentropy};
+  const GradIn in{d_labels, d_lse, d_entropy, d_dlogp, d_dentropy, d_lse_low};
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaSuccess;
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     const LogitView<T> v{static_cast<const T*>(d_logits), rows, stride_k, stride_row, stride_class, (int32_t)classes, FastDiv((uint32_t)rows)};
     const GradOut<T> o{static_cast<T*>(d_dlogits), out_stride_k, out_stride_row, out_stride_class};
-    e = launch_grad<T>(v, in, o, K, stream);
+    e = d_lse_low ? launch_grad<T, true>(v, in, o, K, stream) : launch_grad<T, false>(v, in, o, K, stream);
   });
   return err.done(e);
+}
+
+}  // namespace
+
+extern "C" int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                                 int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
+                                 const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
+                                 void* cuda_stream, char* h_err, size_t h_err_len) {
+  return logprob_grad(Err("lsam_logprob_grad", h_err, h_err_len), d_logits, dtype, K, rows, classes, stride_k, stride_row, stride_class, d_labels, d_lse, nullptr, d_entropy, d_dlogp,
+                      d_dentropy, d_dlogits, out_stride_k, out_stride_row, out_stride_class, cuda_stream);
+}
+
+extern "C" int lsam_logprob_grad_wide(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
+                                      int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_lse_low, const float* d_entropy, const float* d_dlogp,
+                                      const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
+                                      void* cuda_stream, char* h_err, size_t h_err_len) {
+  return logprob_grad(Err("lsam_logprob_grad_wide", h_err, h_err_len), d_logits, dtype, K, rows, classes, stride_k, stride_row, stride_class, d_labels, d_lse, d_lse_low, d_entropy,
+                      d_dlogp, d_dentropy, d_dlogits, out_stride_k, out_stride_row, out_stride_class, cuda_stream);
 }
 
 namespace {
@@ -401,7 +435,7 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
   });
   if (e == cudaSuccess) {
     // programmatic dependent launch: the join's blocks become resident while the tiles drain and wait for them there
-    const ScoreOut out{d_logp, d_lse, d_entropy, nullptr, nullptr, 0};
+    const ScoreOut out{d_logp, d_lse, d_entropy, nullptr, nullptr, 0, nullptr};
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -108,3 +108,13 @@ def test_binding_refuses_what_is_not_a_cuda_tensor_of_the_right_form():
         G.lsam_dropout(x, 0.5, -1, 1)
     with pytest.raises(G.LsamError, match="workers"):  # would wrap in a 32-bit argument
         G.lsam_logprob(torch.zeros(1, 1, 1).expand(1 << 32, 1, 1))
+
+
+def test_two_word_forms_refuse_as_the_others_do():
+    for rc, msg in (_call(G.lib().lsam_logprob_wide, P, 3, 1, 2, 5, 10, 5, 1, P, 0, P, P, P, P, P, P),
+                    _call(G.lib().lsam_logprob_wide, P, 0, 1, 2, 0, 10, 5, 1, P, 0, P, P, P, P, P, P)):
+        assert rc == G.LSAM_ERR_INVALID and msg.startswith("lsam_logprob_wide: ")
+    rc, msg = _call(G.lib().lsam_logprob_grad_wide, P, 0, 1, 2, 5, 10, 5, 1, P, P, P, P, None, None, P, 10, 5, 1)
+    assert rc == G.LSAM_ERR_INVALID and msg.startswith("lsam_logprob_grad_wide: ") and "neither" in msg
+    assert _call(G.lib().lsam_logprob_wide, P, 0, 0, 2, 5, 10, 5, 1, P, 0, P, P, P, P, P, P)[0] == G.LSAM_OK
+    assert _call(G.lib().lsam_logprob_grad_wide, P, 0, 0, 2, 5, 10, 5, 1, P, P, P, P, P, P, P, 10, 5, 1)[0] == G.LSAM_OK
