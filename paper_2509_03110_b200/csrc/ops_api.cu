@@ -309,8 +309,21 @@ struct HeadSpace {
   size_t label, h, w, total;
   int64_t pad;
 };
-HeadSpace head_space(HeadForm f, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool shared_w) {
-  const int64_t parts = f == HEAD_GEMV || f == HEAD_TILES ? share_plan(f, K, rows, classes).splits : 2 * ht_plan(K, rows, classes).runs;
+// The form of a call and how it is split: `share` for GEMV and TILES, `tile` for the tensor cores.
+struct HeadPlan {
+  HeadForm form;
+  SharePlan share;
+  HeadTile tile{};
+};
+HeadPlan head_plan(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool aligned) {
+  HeadPlan p{head_form(dtype, K, rows, inner, classes, aligned)};
+  if (p.form == HEAD_GEMV || p.form == HEAD_TILES) p.share = share_plan(p.form, K, rows, classes);
+  else p.tile = ht_plan(K, rows, classes);
+  return p;
+}
+HeadSpace head_space(const HeadPlan& p, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, bool shared_w) {
+  const HeadForm f = p.form;
+  const int64_t parts = f == HEAD_GEMV || f == HEAD_TILES ? p.share.splits : 2 * p.tile.runs;
   const int64_t planes = dtype == LSAM_FP32 ? 3 : 1;
   HeadSpace s;
   s.pad = round_up(inner, 8);
@@ -367,7 +380,7 @@ cudaError_t launch_copy(CopySide h, CopySide w, int64_t inner, int64_t pad, cuda
 
 extern "C" size_t lsam_head_logprob_workspace_bytes(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, int32_t flags) {
   if (!dtype_ok(dtype) || !head_sizes_ok(K, rows, inner, classes)) return 0;
-  return head_space(head_form(dtype, K, rows, inner, classes, (flags & LSAM_HEAD_ALIGNED) != 0), dtype, K, rows, inner, classes, (flags & LSAM_HEAD_SHARED) != 0 || K == 1).total;
+  return head_space(head_plan(dtype, K, rows, inner, classes, (flags & LSAM_HEAD_ALIGNED) != 0), dtype, K, rows, inner, classes, (flags & LSAM_HEAD_SHARED) != 0 || K == 1).total;
 }
 
 extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
@@ -389,8 +402,9 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (n0 == 1 || (s0 > 0 && s0 * es % 16 == 0)) && (n1 == 1 || (s1 > 0 && s1 * es % 16 == 0));
   };
   const bool h_aligned = aligned16(d_h, K, h_stride_k, rows, h_stride_row), w_aligned = aligned16(d_w, shared ? 1 : K, w_stride_k, classes, w_stride_class);
-  const HeadForm form = head_form(dtype, K, rows, inner, classes, h_aligned && w_aligned);
-  const HeadSpace sp = head_space(form, dtype, K, rows, inner, classes, shared);
+  const HeadPlan plan = head_plan(dtype, K, rows, inner, classes, h_aligned && w_aligned);
+  const HeadForm form = plan.form;
+  const HeadSpace sp = head_space(plan, dtype, K, rows, inner, classes, shared);
   if (workspace_bytes < sp.total) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_head_logprob_workspace_bytes()");
   if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return err.fail(LSAM_ERR_WORKSPACE, "workspace not 256-byte aligned");
   PtrCheck pc;
@@ -406,7 +420,7 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
     using T = decltype(t);
     const T *h = static_cast<const T*>(d_h), *w = static_cast<const T*>(d_w);
     if (form == HEAD_GEMV || form == HEAD_TILES) {
-      const SharePlan p = share_plan(form, K, rows, classes);
+      const SharePlan& p = plan.share;
       a.parts = p.splits;
       a.per_split = p.per_split;
       if (form == HEAD_GEMV) {
@@ -417,7 +431,7 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
       }
       return;
     }
-    const HeadTile q = ht_plan(K, rows, classes);
+    const HeadTile& q = plan.tile;
     a.parts = 2 * q.runs;
     if (form == HEAD_COPY) {
       using D = typename std::conditional<sizeof(T) == 4, bf16, T>::type;

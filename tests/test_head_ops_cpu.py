@@ -1,5 +1,8 @@
 """Refusals of the operators around a classifier's head that need no GPU: every bad argument is turned into an error code on the host."""
 import ctypes as C
+import math
+import random
+from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 import torch
@@ -118,3 +121,32 @@ def test_two_word_forms_refuse_as_the_others_do():
     assert rc == G.LSAM_ERR_INVALID and msg.startswith("lsam_logprob_grad_wide: ") and "neither" in msg
     assert _call(G.lib().lsam_logprob_wide, P, 0, 0, 2, 5, 10, 5, 1, P, 0, P, P, P, P, P, P)[0] == G.LSAM_OK
     assert _call(G.lib().lsam_logprob_grad_wide, P, 0, 0, 2, 5, 10, 5, 1, P, P, P, P, P, P, P, 10, 5, 1)[0] == G.LSAM_OK
+
+
+def _runs(K, rows, classes):
+    """Runs of tiles per row tile by the whole search: falling widths, then falling runs, the first of equals."""
+    pair = rows > 128
+    ctas, m = (74, -(-rows // 256)) if pair else (148, -(-rows // 128))
+    best = None
+    for n in range(256, 31, -32 if pair else -16):
+        tiles_n = -(-classes // n)
+        for run in range(min(tiles_n, 32), 0, -1):
+            runs = -(-tiles_n // run)
+            tiles = float(-(-K * m * runs // ctas) * run)
+            cost = (tiles * (n + 32) if pair else tiles * (n + 8) + 0.25 * n) * (1.0 + 0.02 / run)
+            if best is None or cost < best[0]:
+                best = cost, runs
+    return best[1]
+
+
+def test_the_plan_of_a_head_call_is_the_best_of_all_and_a_function_of_its_sizes():
+    rng = random.Random(0)
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))  # noqa: E731
+    sizes = [(log(1, 64), log(1, 8192), log(1, 300000)) for _ in range(250)] + [(1, 4, 32768), (32, 256, 1000), (1, 4096, 32768), (1, 128, 1 << 30), (3, 129, 1)]
+    f = G.lib().lsam_head_logprob_workspace_bytes
+    up = lambda v: -(-v // 256) * 256  # noqa: E731
+    want = [up(12 * 2 * _runs(*s) * s[0] * s[1]) + up(4 * s[0] * s[1]) for s in sizes]
+    ask = lambda _: [f(G.BF16, K, rows, 64, classes, G.HEAD_ALIGNED) for K, rows, classes in sizes]  # noqa: E731
+    assert ask(0) == want
+    with ThreadPoolExecutor(4) as pool:
+        assert all(got == want for got in pool.map(ask, range(8)))
