@@ -385,6 +385,7 @@ int lsam_logprob_grad_wide(const void* d_logits, int32_t dtype, int32_t K, int64
  *  the GPU (other streams, graphs replayed side by side) need one each.  flags of the query: LSAM_HEAD_ALIGNED = addresses of h and w and
  *  the strides of their dimensions of more than one element are multiples of 16 bytes, and none of them 0 but w_stride_k; LSAM_HEAD_SHARED =
  *  w_stride_k is 0.  The query is host-only and returns 0 for sizes that the call refuses.
+ * Every wait in the kernels is bounded.  One that runs out is not an error code (the call has returned by then): the rows it concerns come back as NaN.
  * K <= 65535, rows <= 4194240, inner and classes <= 2^30. */
 enum { LSAM_HEAD_ALIGNED = 1, LSAM_HEAD_SHARED = 2 };
 size_t lsam_head_logprob_workspace_bytes(int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, int32_t flags);
@@ -392,6 +393,12 @@ int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int
                       int64_t h_stride_k, int64_t h_stride_row, int64_t w_stride_k, int64_t w_stride_class, int64_t bias_stride_k,
                       const int32_t* d_labels, float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes,
                       void* cuda_stream, char* h_err, size_t h_err_len);
+
+/* Self-test: lsam_head_logprob of dense h and w in the kernels' tensor-core form, none of whose copies is ever issued: every wait for one runs out after a
+ * short limit, and every row that is not left out comes back as NaN. */
+int lsam_selftest_head_wait(const void* d_h, const void* d_w, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, const int32_t* d_labels,
+                            float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* h_err,
+                            size_t h_err_len);
 
 /* Dropout with a mask that is never stored:  out = skip + (kept ? x * scale : 0)  (skip NULL: 0), x, skip and out [K, rows, n] of `dtype`,
  * columns contiguous.  Whether column c of row r of worker k_offset + k is kept is a function of (seed, tick, layer, worker, r, c) alone, so the ascent

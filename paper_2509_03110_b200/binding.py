@@ -29,7 +29,7 @@ EXPORTS = [
     "lsam_profile_enable", "lsam_profile_read", "lsam_launch_count", "lsam_uses_tcgen05", "lsam_last_error",
     "lsam_destroy", "lsam_schedule_hash", "lsam_row_norms_static", "lsam_acc_buffer", "lsam_selftest_bounded_wait",
     "lsam_checkpoint_bytes", "lsam_save_checkpoint", "lsam_load_checkpoint", "lsam_read_anchor_gap",
-    "lsam_logprob", "lsam_logprob_grad", "lsam_logprob_wide", "lsam_logprob_grad_wide", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout", "lsam_score_batch",
+    "lsam_logprob", "lsam_logprob_grad", "lsam_logprob_wide", "lsam_logprob_grad_wide", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout", "lsam_score_batch", "lsam_selftest_head_wait",
 ]
 
 
@@ -118,6 +118,7 @@ def lib():
     L.lsam_head_logprob_workspace_bytes.restype = C.c_size_t
     L.lsam_head_logprob_workspace_bytes.argtypes = [i32, i32, i64, i64, i64, i32]
     L.lsam_head_logprob.argtypes = [vp, vp, vp, i32, i32] + [i64] * 8 + [vp] * 5 + [C.c_size_t] + err
+    L.lsam_selftest_head_wait.argtypes = [vp, vp, i32, i32] + [i64] * 3 + [vp] * 5 + [C.c_size_t] + err
     L.lsam_dropout.argtypes = [vp, vp, vp, i32, i32] + [i64] * 8 + [C.c_double, C.c_uint64, C.c_uint64, i32, i32] + err
     _lib = L
     return L

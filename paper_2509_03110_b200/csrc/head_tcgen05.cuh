@@ -10,7 +10,7 @@
 //   single CTA (up to 128 rows): the bytes of w bound it; only the rows that exist are loaded (the others' accumulator rows are never read).
 // tile_n, a multiple of 32 (single CTAs: 16) up to 256, is the width that loads all SMs evenly.  The work list has the row tile fastest: the CTAs that run together
 // read the same few tiles of w, so w crosses HBM once, whatever the number of row tiles.
-// All waits are bounded as in gemm_tcgen05.cuh; a CTA that gives up leaves NaN statistics for its rows.
+// All waits are bounded as in gemm_tcgen05.cuh; a CTA that gives up leaves NaN statistics for its rows, and NaN for the logits of their labels.
 #pragma once
 
 #include <algorithm>
@@ -60,8 +60,9 @@ __device__ inline bool ht_elect() {
   asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
   return p != 0;
 }
+template <uint32_t LIMIT>
 __device__ inline bool ht_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  for (uint32_t i = 0; i < tc::kSpinLimit; ++i) {
+  for (uint32_t i = 0; i < LIMIT; ++i) {
     uint32_t ok;
     asm volatile(
         "{\n"
@@ -138,9 +139,11 @@ __device__ __forceinline__ void ht_block_stats(float (&l)[32], RowStat& st, int6
 
 // fp32 operands arrive as three bf16 planes each (head_copy_kernel) and six products of planes are accumulated, as in the fp32 models' GEMMs.
 // grid: CTAs (pairs: clusters of 2), each walking units u, u + grid, ...; unit = (run of class tiles, row tile) of a worker, row tile fastest
-template <bool PAIR>
+// STARVED (self-test): no copy is ever issued and the waits are short, so all of them run out with nothing in flight.
+template <bool PAIR, bool STARVED>
 __global__ void __launch_bounds__(kHtThreads, 1)
 head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_constant__ CUtensorMap map_w, HeadArgs a, HeadTile q) {
+  constexpr uint32_t LIMIT = STARVED ? 1u << 13 : tc::kSpinLimit;
   const int STAGES = q.stages, A_BYTES = q.a_bytes, STAGE = q.stage_bytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -183,7 +186,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHtRegsIssue));
     const bool one = ht_elect();
-    if (warp == 0 && (PAIR || one)) {
+    if (!STARVED && warp == 0 && (PAIR || one)) {
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
@@ -201,7 +204,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
             const int pa = q.pairs == 1 ? 0 : pp < 3 ? pp : pp < 5 ? pp - 3 : 0, pb = q.pairs == 1 ? 0 : pp < 3 ? 2 - pp : pp < 5 ? 4 - pp : 0;
             const int zh = k + pa * q.K, zw = q.w_shared ? pb : kw + pb * q.K;
             for (int kb = 0; kb < k_blocks; ++kb) {
-              if (!ht_wait(empty0 + 8 * s, ph ^ 1u, abort_flag)) { ok = false; break; }
+              if (!ht_wait<LIMIT>(empty0 + 8 * s, ph ^ 1u, abort_flag)) { ok = false; break; }
               const uint32_t dst = ring0 + s * STAGE;
               if (!PAIR || one) {
                 if (!PAIR || leader) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full0 + 8 * s), "r"(tx) : "memory");
@@ -227,10 +230,10 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
           int in_chunk = 0;
           for (int kb = 0; kb < k_total; ++kb) {
             if (in_chunk == 0) {
-              if (!ht_wait(acc_empty0 + 8 * as, aph ^ 1u, abort_flag)) { ok = false; break; }
+              if (!ht_wait<LIMIT>(acc_empty0 + 8 * as, aph ^ 1u, abort_flag)) { ok = false; break; }
               tc::tc_fence_after();
             }
-            if (!ht_wait(full0 + 8 * s, ph, abort_flag)) { ok = false; break; }
+            if (!ht_wait<LIMIT>(full0 + 8 * s, ph, abort_flag)) { ok = false; break; }
             const uint32_t d = tmem_base + (uint32_t)as * kHtMaxN, a_lo = lo0 + s * step, b_lo = a_lo + b_off;
             const bool last = in_chunk == kHtChunk - 1 || kb == k_total - 1;
             if (!PAIR || one) {
@@ -280,7 +283,7 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
           bv[b] = bias && c < nv ? __ldg(bias + c_tile + c) : 0.f;
         }
         for (int ch = 0; ch < chunks && ok; ++ch) {
-          if (!tc::mbar_wait(&acc_full[as], aph, abort_flag)) { ok = false; break; }
+          if (!tc::mbar_wait_limit(&acc_full[as], aph, abort_flag, LIMIT)) { ok = false; break; }
           tc::tc_fence_after();
           const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)as * kHtMaxN;
           if (ch == 0) {  // all of them in flight at once
@@ -328,6 +331,8 @@ head_tcgen05_kernel(const __grid_constant__ CUtensorMap map_h, const __grid_cons
       if (!ok) {
         *abort_flag = 1;
         st = {0.f, NAN, NAN};
+        // nobody may have written the logit of a label in these classes: what is there is the workspace's, and must not pass for a mask
+        if (live && y >= (int64_t)rn * q.run * q.tile_n && y < (int64_t)nt_end * q.tile_n) a.at_label[i] = NAN;
       }
       if (live) a.part[(int64_t)(rn * 2 + half) * a.total + i] = st;
     }
@@ -413,7 +418,7 @@ inline bool ht_make_map(CUtensorMap* m, const T* base, uint64_t inner, uint64_t 
 
 // False (nothing launched): the operands' addresses or strides are not what TMA takes.  *e: the launch's error.
 template <typename T>
-inline bool ht_launch(const T* h, const T* w, HeadArgs a, int32_t K, HeadTile q, int planes, bool shared, cudaStream_t stream, cudaError_t* e) {
+inline bool ht_launch(const T* h, const T* w, HeadArgs a, int32_t K, HeadTile q, int planes, bool shared, bool starved, cudaStream_t stream, cudaError_t* e) {
   const bool pair = a.rows > kHtRows;
   CUtensorMap mh, mw;
   q.w_shared = shared;
@@ -424,7 +429,8 @@ inline bool ht_launch(const T* h, const T* w, HeadArgs a, int32_t K, HeadTile q,
   q.idesc = tc::instr_desc(pair ? 256 : 128, q.tile_n, false, false);
   if (!std::is_same<T, bf16>::value) q.idesc &= ~((1u << 7) | (1u << 10));  // operands f16 instead of bf16
   a.parts = 2 * q.runs;
-  const void* kern = pair ? (const void*)head_tcgen05_kernel<true> : (const void*)head_tcgen05_kernel<false>;
+  const void* kern = starved ? (pair ? (const void*)head_tcgen05_kernel<true, true> : (const void*)head_tcgen05_kernel<false, true>)
+                             : (pair ? (const void*)head_tcgen05_kernel<true, false> : (const void*)head_tcgen05_kernel<false, false>);
   const int smem = kHtSmem;
   if ((*e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return true;
   cudaLaunchConfig_t cfg = {};

@@ -383,11 +383,11 @@ extern "C" size_t lsam_head_logprob_workspace_bytes(int32_t dtype, int32_t K, in
   return head_space(head_plan(dtype, K, rows, inner, classes, (flags & LSAM_HEAD_ALIGNED) != 0), dtype, K, rows, inner, classes, (flags & LSAM_HEAD_SHARED) != 0 || K == 1).total;
 }
 
-extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
-                                 int64_t h_stride_k, int64_t h_stride_row, int64_t w_stride_k, int64_t w_stride_class, int64_t bias_stride_k,
-                                 const int32_t* d_labels, float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes,
-                                 void* cuda_stream, char* h_err, size_t h_err_len) {
-  const Err err("lsam_head_logprob", h_err, h_err_len);
+namespace {
+
+int head_logprob(const Err& err, const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
+                 int64_t h_stride_k, int64_t h_stride_row, int64_t w_stride_k, int64_t w_stride_class, int64_t bias_stride_k, const int32_t* d_labels, float* d_logp,
+                 float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes, bool starved, void* cuda_stream) {
   if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
   if (K < 0 || rows < 0 || inner < 1 || classes < 1 || classes > kMaxHead || inner > kMaxHead)
     return err.fail(LSAM_ERR_INVALID, "need K >= 0, rows >= 0, 1 <= inner, classes <= 2^30");
@@ -404,6 +404,7 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
   const bool h_aligned = aligned16(d_h, K, h_stride_k, rows, h_stride_row), w_aligned = aligned16(d_w, shared ? 1 : K, w_stride_k, classes, w_stride_class);
   const HeadPlan plan = head_plan(dtype, K, rows, inner, classes, h_aligned && w_aligned);
   const HeadForm form = plan.form;
+  if (starved && form != HEAD_TENSOR) return err.fail(LSAM_ERR_INVALID, "these operands do not go to the tensor cores as they are");
   const HeadSpace sp = head_space(plan, dtype, K, rows, inner, classes, shared);
   if (workspace_bytes < sp.total) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_head_logprob_workspace_bytes()");
   if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return err.fail(LSAM_ERR_WORKSPACE, "workspace not 256-byte aligned");
@@ -442,9 +443,9 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
       a.hr = a.wr = sp.pad;
       a.hk = rows * sp.pad;
       a.wk = classes * sp.pad;
-      if (!ht_launch<D>(hc, wc, a, K, q, planes, shared, stream, &e)) e = cudaErrorInvalidValue;
+      if (!ht_launch<D>(hc, wc, a, K, q, planes, shared, false, stream, &e)) e = cudaErrorInvalidValue;
     } else if constexpr (sizeof(T) == 2) {
-      if (!ht_launch<T>(h, w, a, K, q, 1, shared, stream, &e)) e = cudaErrorInvalidValue;
+      if (!ht_launch<T>(h, w, a, K, q, 1, shared, starved, stream, &e)) e = cudaErrorInvalidValue;
     }
   });
   if (e == cudaSuccess) {
@@ -458,6 +459,23 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
     e = cudaLaunchKernelEx(&cfg, head_join_kernel, a, total, out);
   }
   return err.done(e);
+}
+
+}  // namespace
+
+extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* d_bias, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes,
+                                 int64_t h_stride_k, int64_t h_stride_row, int64_t w_stride_k, int64_t w_stride_class, int64_t bias_stride_k,
+                                 const int32_t* d_labels, float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes,
+                                 void* cuda_stream, char* h_err, size_t h_err_len) {
+  return head_logprob(Err("lsam_head_logprob", h_err, h_err_len), d_h, d_w, d_bias, dtype, K, rows, inner, classes, h_stride_k, h_stride_row, w_stride_k, w_stride_class,
+                      bias_stride_k, d_labels, d_logp, d_lse, d_entropy, d_workspace, workspace_bytes, false, cuda_stream);
+}
+
+extern "C" int lsam_selftest_head_wait(const void* d_h, const void* d_w, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, const int32_t* d_labels,
+                                       float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* h_err,
+                                       size_t h_err_len) {
+  return head_logprob(Err("lsam_selftest_head_wait", h_err, h_err_len), d_h, d_w, nullptr, dtype, K, rows, inner, classes, rows * inner, inner, classes * inner, inner, 0, d_labels,
+                      d_logp, d_lse, d_entropy, d_workspace, workspace_bytes, true, cuda_stream);
 }
 
 namespace {
