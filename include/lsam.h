@@ -328,7 +328,8 @@ int lsam_row_norms_static(const float* d_g, int64_t ld, int64_t n, int32_t K, fl
  *  - d_* pointers are memory of the CURRENT device, aligned to their element type (checked: LSAM_ERR_INVALID, nothing is launched).
  *  - Tensors of workers are stacked: index (k, row, column), strides in elements.  K = 1 for a single model.  Per-row arrays
  *    (labels, logp, lse, ...) are dense [K, rows].  K = 0 or rows = 0 is a valid call that does nothing.
- *  - Arithmetic in fp32 whatever the storage type; one rounding at the end where the result is stored in 16 bits.
+ *  - Arithmetic in fp32 whatever the storage type; one rounding at the end where the result is stored in 16 bits.  Exponentials come from the
+ *    special-function unit: e^x is off by a factor of 1 +- (2^-22 + 3 |x| 2^-24), x = l - max l or l - lse.
  *  - h_err: nullable host buffer of h_err_len bytes that receives a message when the call fails. */
 enum { LSAM_FP32 = 0, LSAM_BF16 = 1, LSAM_FP16 = 2 };
 
@@ -360,7 +361,8 @@ int lsam_logprob_wide(const void* d_logits, int32_t dtype, int32_t K, int64_t ro
  * (nullable: 0; not both NULL; dlogp needs d_labels, dentropy needs d_entropy).  The minibatch cross-entropy of a context is
  * dlogp = -1 / batch.  Rows that are left out (negative label) and rows of nothing but masks (lse = -inf) get zeros, whatever else they
  * hold; in any other row a label >= classes makes the row NaN.
- * d_dlogits: type of the logits, strides of its own (every dimension steps over all that the smaller strides span); may be d_logits itself with the same strides. */
+ * d_dlogits: type of the logits, strides of its own (every dimension steps over all that the smaller strides span); may be d_logits itself with the same strides,
+ * else it must not overlap it. */
 int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                       int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_entropy, const float* d_dlogp,
                       const float* d_dentropy, void* d_dlogits, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_class,
@@ -377,7 +379,8 @@ int lsam_logprob_grad_wide(const void* d_logits, int32_t dtype, int32_t K, int64
 /* The first three results of lsam_logprob for the logits l = h w^T + bias, which are never stored:
  *  d_h [K, rows, inner] and d_w [K, classes, inner] of `dtype`, the inner index contiguous; w_stride_k = 0 shares one head among the workers.
  *  d_bias [K, classes] fp32 (bias_stride_k, 0 = shared) or NULL.  Labels and results as in lsam_logprob.
- * Products are accumulated in fp32.  16-bit operands whose addresses and strides are multiples of 16 bytes go to the tensor cores as they are;
+ * Products are accumulated in fp32; the tensor cores cut off what lies below an accumulator's last place, so sums go in chunks of 768 inner indices that are
+ * added in registers (a logit is off by about 3e-7 of the sum of its terms' magnitudes at 4096 inner indices, two to three times an fp32 product).  16-bit operands whose addresses and strides are multiples of 16 bytes go to the tensor cores as they are;
  * others are first copied into the workspace (fp32 as three bf16 planes, whose six leading products keep fp32 accuracy), except small products and
  * at most eight rows, which stay on the FMA pipes.  Classes are masked through the bias: an fp32 element of h or w that is infinite, or above 3.38e38,
  * the largest bf16, may turn the logits it enters into NaN.

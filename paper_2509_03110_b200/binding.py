@@ -174,6 +174,7 @@ def lsam_row_norms_static(g, n, out, stream=None):
 
 
 # ---- operators around a classifier's head (include/lsam.h, last section)
+# Plain calls on tensors: autograd records none of them and does not see what is written through `out`.
 FP32, BF16, FP16 = 0, 1, 2
 HEAD_ALIGNED, HEAD_SHARED = 1, 2
 TOP_MAX, DROPOUT_LAYERS, DROPOUT_WORKERS = 32, 4096, 1 << 20

@@ -107,8 +107,8 @@ cudaError_t launch_row(const LogitView<T>& v, const int32_t* labels, const Score
 }
 
 // Which form a call takes.  Many rows of few classes: a thread per row, from 32768 rows of up to 256 classes with the sample index contiguous (106647
-// rows of 95 bf16: 87 us in the feature kernel, 10 with a thread per row; 5 alternatives 41), from 4096 rows of up to 64 contiguous classes (60000 rows
-// of 10 fp32: 5 us), unless the alternatives, a walk over the row each, cost more (8192 rows of 64, 8 alternatives: 47 us against a warp's 20).  Other
+// rows of 95 bf16: 87 us in the feature kernel, 9 with a thread per row; 5 alternatives 40), from 4096 rows of up to 64 contiguous classes (60000 rows
+// of 10 fp32: 3 us), unless the alternatives, a walk over the row each, cost more (8192 rows of 64, 8 alternatives: 47 us against a warp's 13).  Other
 // sample-contiguous logits go to the feature kernel.  Rows of contiguous classes: a warp per row up to 1024 classes, 128 threads up to 32 KB, 256 beyond;
 // rows of 32 KB and more that leave most of the machine idle are split over a cluster of 8 or 4 blocks (4 rows of 131072 bf16, 8 alternatives: 14.4 us
 // with one block a row, 8.3 with eight; 64 rows: 14.4, four blocks 10.7).
@@ -281,7 +281,7 @@ namespace {
 //   COPY    the rest: copied into aligned rows (fp32: three bf16 planes), then the tensor cores.
 // A step of TILES takes 0.8 to 1.7 us, whatever the rows; COPY has one launch more and moves both matrices.  Measured (us, TILES / COPY), bf16 rows x inner x
 // classes: 16 x 20 x 1000 7.4 / 8.9, 300 x 20 x 1000 7.7 / 11.2, 16 x 101 x 70 11.8 / 8.1, 82 x 301 x 1000 24 / 10.7, 82 x 1091 x 70 70 / 11.7, 2000 x 1021 x 16384
-// 4297 / 98;  fp32: 40 x 8 x 20001 12 / 33, 101 x 394 x 1722 31 / 19.8;  4 x 4096 x 32768 fp32 in tiles 287, GEMV 102.
+// 4297 / 96;  fp32: 40 x 8 x 20001 12 / 33, 101 x 394 x 1722 31 / 19.8;  4 x 4096 x 32768 fp32 in tiles 287, GEMV 102.
 enum HeadForm { HEAD_TENSOR, HEAD_GEMV, HEAD_COPY, HEAD_TILES };
 constexpr int64_t kTileSteps = 4;
 // GEMV and TILES: shares of the classes, enough to occupy the machine, none shorter than what a block takes at a time.
