@@ -326,7 +326,10 @@ struct lsam_ctx {
   // the calls that touch the GPU want the context's device to be the current one
   int check_device() {
     int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess) return fail(LSAM_ERR_CUDA, "cudaGetDevice failed");
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return fail(LSAM_ERR_CUDA, "cudaGetDevice failed");
+    }
     if (dev != device) return fail(LSAM_ERR_INVALID, "the context lives on device " + std::to_string(device) + " but device " + std::to_string(dev) + " is current");
     return LSAM_OK;
   }
@@ -339,11 +342,14 @@ struct lsam_ctx {
 
 namespace {
 
+// A failed call is reported once: the runtime's last error is taken back, or the next launch anywhere in the library would be blamed for it.
 #define LSAM_CUDA(ctx, call)                                                                          \
   do {                                                                                                \
     cudaError_t e__ = (call);                                                                         \
-    if (e__ != cudaSuccess)                                                                           \
+    if (e__ != cudaSuccess) {                                                                         \
+      (void)cudaGetLastError();                                                                       \
       return (ctx)->fail(LSAM_ERR_CUDA, std::string(#call) + ": " + cudaGetErrorString(e__));         \
+    }                                                                                                 \
   } while (0)
 
 int prof_begin(lsam_ctx* c, int cls) {
@@ -1096,6 +1102,7 @@ int graph_capture(lsam_ctx* c, lsam_ctx::GraphSlot& gs, float eta, float rho, bo
   const cudaError_t e = cudaStreamEndCapture(c->stream, &graph);
   if (rc != LSAM_OK || e != cudaSuccess || !graph) {
     if (graph) cudaGraphDestroy(graph);
+    (void)cudaGetLastError();
     return rc != LSAM_OK ? rc : c->fail(LSAM_ERR_CUDA, std::string("cudaStreamEndCapture: ") + cudaGetErrorString(e));
   }
   gs.launches = c->launches - l0;
@@ -1232,7 +1239,11 @@ int lsam_init(lsam_ctx** out, const lsam_config* cfg, const void* d_X, const voi
   c->t_x.assign(cfg->K, 0);
   c->async_on = cfg->active_num > 0 && cfg->active_num < 256;
   c->active_host.assign(cfg->K, 1);
-  auto bail = [&](int code) { delete c; return code; };
+  auto bail = [&](int code) {
+    if (code == LSAM_ERR_CUDA) (void)cudaGetLastError();
+    delete c;
+    return code;
+  };
   // tensor-core path: decided once per context
   const bool mlp = cfg->model == LSAM_MODEL_MLP || cfg->model == LSAM_MODEL_RESMLP;
   bool tc_ok = false;
@@ -1280,7 +1291,7 @@ int lsam_init(lsam_ctx** out, const lsam_config* cfg, const void* d_X, const voi
     std::vector<TcLayer> tl;
     for (const LayerInfo& li : L.layers) tl.push_back({li.in, li.out, li.w_pad, li.b_pad, li.residual});
     std::string why;
-    if (tc_plan(c->tc, *cfg, tl, b, &c->launches, why) != 0) { delete c; return LSAM_ERR_CUDA; }
+    if (tc_plan(c->tc, *cfg, tl, b, &c->launches, why) != 0) return bail(LSAM_ERR_CUDA);
   }
   *out = c;
   return LSAM_OK;
@@ -1801,6 +1812,7 @@ float* g_static_partials_addr[kMaxDevices] = {};  // device address of the array
 
 int static_fail(int code, const char* msg, char* h_err, size_t h_err_len) {
   if (h_err && h_err_len > 0) std::snprintf(h_err, h_err_len, "%s", msg);
+  if (code == LSAM_ERR_CUDA) (void)cudaGetLastError();
   return code;
 }
 }  // namespace
