@@ -474,8 +474,9 @@ extern "C" int lsam_head_logprob(const void* d_h, const void* d_w, const float* 
 extern "C" int lsam_selftest_head_wait(const void* d_h, const void* d_w, int32_t dtype, int32_t K, int64_t rows, int64_t inner, int64_t classes, const int32_t* d_labels,
                                        float* d_logp, float* d_lse, float* d_entropy, void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* h_err,
                                        size_t h_err_len) {
-  return head_logprob(Err("lsam_selftest_head_wait", h_err, h_err_len), d_h, d_w, nullptr, dtype, K, rows, inner, classes, rows * inner, inner, classes * inner, inner, 0, d_labels,
-                      d_logp, d_lse, d_entropy, d_workspace, workspace_bytes, true, cuda_stream);
+  const bool ok = head_sizes_ok(K, rows, inner, classes);  // sizes that are refused need no strides
+  return head_logprob(Err("lsam_selftest_head_wait", h_err, h_err_len), d_h, d_w, nullptr, dtype, K, rows, inner, classes, ok ? rows * inner : 0, inner, ok ? classes * inner : 0, inner, 0,
+                      d_labels, d_logp, d_lse, d_entropy, d_workspace, workspace_bytes, true, cuda_stream);
 }
 
 namespace {

@@ -150,3 +150,12 @@ def test_the_plan_of_a_head_call_is_the_best_of_all_and_a_function_of_its_sizes(
     assert ask(0) == want
     with ThreadPoolExecutor(4) as pool:
         assert all(got == want for got in pool.map(ask, range(8)))
+
+
+def test_the_self_test_of_the_waits_refuses_as_the_call_does():
+    f = G.lib().lsam_selftest_head_wait
+    call = lambda dtype, K, rows, inner, classes: _call(f, P, P, dtype, K, rows, inner, classes, P, P, P, P, P, 1 << 20)  # noqa: E731
+    for kw, word in (((5, 1, 2, 8, 5), "dtype"), ((1, 1, 2, 0, 5), "inner"), ((1, 1, 1 << 62, 8, 5), "rows"), ((1, 1, 2, 1 << 62, 5), "2^30"), ((1, 1, 2, 8, 1 << 62), "2^30"), ((0, 1, 2, 8, 5), "tensor cores")):
+        rc, msg = call(*kw)
+        assert rc == G.LSAM_ERR_INVALID and word in msg and msg.startswith("lsam_selftest_head_wait: "), (kw, msg)
+    assert call(1, 0, 2, 8, 5)[0] == G.LSAM_OK
