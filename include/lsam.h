@@ -369,7 +369,7 @@ int lsam_logprob_grad(const void* d_logits, int32_t dtype, int32_t K, int64_t ro
                       void* cuda_stream, char* h_err, size_t h_err_len);
 
 /* The same with both words of lsam_logprob_wide: p_c = e^(l[c] - lse - lse_low).  With lse alone every p_c of a row is off by a factor of
- * 1 +- |lse| 2^-24: nothing to speak of for usual logits, 1.6e-4 in fp32 rows around 1e4 (whose logits are themselves that far apart), and no
+ * 1 +- |lse| 2^-24: nothing to speak of for usual logits, up to 6e-4 in fp32 rows around 1e4 (whose logits are themselves 1e-3 apart), and no
  * distribution any more where all logits are large, such as a row that an additive mask of -1e9 has emptied.  d_lse_low: nullable (0). */
 int lsam_logprob_grad_wide(const void* d_logits, int32_t dtype, int32_t K, int64_t rows, int64_t classes, int64_t stride_k, int64_t stride_row,
                            int64_t stride_class, const int32_t* d_labels, const float* d_lse, const float* d_lse_low, const float* d_entropy,

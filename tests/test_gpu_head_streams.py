@@ -1,5 +1,7 @@
 """The operators around a classifier's head on a stream that is not the inputs' own: an input that is dropped after the call keeps its memory until the
 stream has read it."""
+from concurrent.futures import ThreadPoolExecutor
+
 import pytest
 import torch
 
@@ -59,3 +61,46 @@ def test_a_dropped_result_buffer_keeps_its_memory():
         assert other.data_ptr() != at
         torch.cuda.synchronize()
         assert not other.any()
+
+
+def test_a_second_stream_inside_a_captured_graph():
+    for name, (run, inputs) in calls().items():
+        want = run(inputs)
+        main, side = torch.cuda.Stream(), torch.cuda.Stream()
+        warm = run(inputs, stream=side)
+        torch.cuda.synchronize()
+        del warm
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=main):
+            mine = {k: v.clone() for k, v in inputs.items()}
+            side.wait_stream(main)
+            got = run(mine, stream=side)
+            del mine  # their memory belongs to the graph, and is not used again in it before the side stream has read it
+            other = [torch.full_like(v, 9) for v in inputs.values()]
+            main.wait_stream(side)
+        for _ in range(3):
+            for v in got:
+                v.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(got, want)), name
+        del other
+
+
+def test_calls_of_several_threads_at_once():
+    table = calls()
+    want = {name: run(inputs) for name, (run, inputs) in table.items()}
+    torch.cuda.synchronize()
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                for name, (run, inputs) in table.items():
+                    got = run(inputs)
+                    stream.synchronize()
+                    assert all(torch.equal(p, q) for p, q in zip(got, want[name])), name
+        return True
+
+    with ThreadPoolExecutor(4) as pool:
+        assert all(pool.map(work, range(4)))
