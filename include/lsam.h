@@ -491,10 +491,9 @@ int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* out, const 
  * (a, b, c) = (3.4445, -4.7750, 2.0315) and 5 steps, those of the Muon optimiser, singular values from 0.003 |G|_F up end between 0.68 and 1.21.
  *  d_g [K, rows, cols] of `dtype`, any strides >= 0; d_out [K, rows, cols] of `dtype`, any strides; it may be d_g itself with the same strides,
  *  else it must not overlap it.  One matrix per worker, each normed by itself; a matrix of zeros stays zero (eps > 0).
- * Products of fp32 accuracy (two fp16 planes of every matrix, three products of planes, fp32 sums); an element of X_t is held to 2^-24 of itself or 2^-38 of the
- * largest singular value that the coefficients allow at that step, whichever is more.  Up to 32 rows or columns: in double throughout.  Results in bf16 of matrices whose
- * smaller side is 512 or more take one product of planes in most places: off by about 1e-3 of the result's norm (rounding to bf16: 1.7e-3), and by up to 2e-2 of itself in a
- * direction that holds most of the norm of G; ask for fp32 where that matters.  A NaN or an infinity in a matrix makes all of it NaN, and so does a matrix of zeros with eps = 0.
+ * Products of fp32 accuracy whatever the type (two fp16 planes of every matrix, three products of planes, fp32 sums); an element of X_t is held to 2^-24 of itself or 2^-38 of the
+ * largest singular value that the coefficients allow at that step, whichever is more.  Up to 32 rows or columns: in double throughout.  The steps carry errors on as they do in a chain of plain fp32
+ * products (with the coefficients above: 1e-6 to 1e-5 of the result's norm); coefficients that do not let singular values settle enlarge them at every step.  A NaN or an infinity in a matrix makes all of it NaN, and so does a matrix of zeros with eps = 0.
  *  d_workspace: lsam_orthogonalize_workspace_bytes() bytes.
  * K <= 65535, rows, cols <= 2^20, steps 0 .. 32, eps >= 0, scale 0 or |scale| >= 2^-90, |a| >= 1 (small singular values have to grow); coefficients for which no bound of the singular values below
  * 2^10 holds throughout are refused. */

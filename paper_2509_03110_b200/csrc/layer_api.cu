@@ -622,10 +622,8 @@ extern "C" int lsam_orthogonalize(const void* d_g, int32_t dtype, int32_t K, int
       const double next = ortho_reach(a, b, c, top);
       const int ea = ortho_exponent(top * top), ep = ortho_exponent(ortho_reach_square(b, c, top * top) + std::fabs((double)a)), en = ortho_exponent(next);
       const auto two = [](int v) { return (float)std::ldexp(1.0, v); };
-      // planes that enter the products: see the head of the kernels' file
-      const bool fine = !std::is_same<T, bf16>::value || m < kNsCoarse, here = fine || s + 2 == steps;
       NsGemm w{};
-      w.m = w.n = (int)m; w.inner = (int)n; w.na = w.nb = fine ? 2 : 1; w.half_result = !std::is_same<T, float>::value;
+      w.m = w.n = (int)m; w.inner = (int)n;
       w.f = two(ea - 2 * ex);
       w.out = A;
       if (q.splits > 1) {
@@ -641,20 +639,19 @@ extern "C" int lsam_orthogonalize(const void* d_g, int32_t dtype, int32_t K, int
         e = ns_launch<fp16, NS_GRAM>(x, x, w, K, stream);
       }
       if (e != cudaSuccess) return;
-      w.inner = (int)m; w.na = w.nb = here ? 2 : 1;
-      // where all products enter, the term a X of the last one is the diagonal of P
-      const bool folded = here;
-      w.f = c * two(ep - 2 * ea); w.h = b * two(ep - ea); w.diagonal = folded ? a * two(ep) : 0.f;
+      w.inner = (int)m;
+      // the term a X of the last product is the diagonal of P
+      w.f = c * two(ep - 2 * ea); w.h = b * two(ep - ea); w.diagonal = a * two(ep);
       w.other = A; w.out = P;
       e = ns_launch<fp16, NS_SQUARE>(A, A, w, K, stream);
       if (e != cudaSuccess) return;
       w.n = (int)n;
-      w.other = x; w.out = y;
+      w.out = y;
       if (s + 1 < steps) {
-        w.f = two(en - ep - ex); w.h = folded ? 0.f : a * two(en - ex);
+        w.f = two(en - ep - ex);
         e = ns_launch<fp16, NS_APPLY>(P, x, w, K, stream);
       } else {
-        w.f = scale * two(-ep - ex); w.h = folded ? 0.f : scale * a * two(-ex);
+        w.f = scale * two(-ep - ex);
         w.final_out = out; w.ok = out_stride_k; w.oi = oi; w.oj = oj;
         e = ns_launch<T, NS_FINAL>(P, x, w, K, stream);
       }

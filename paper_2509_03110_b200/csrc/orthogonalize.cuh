@@ -12,16 +12,11 @@
 // below.  A product takes three products of planes, hi hi + lo hi + hi lo, what is left out being 2^-24 of each term: fp32 accuracy for half of what three
 // bf16 planes and six products cost.  The tensor core cuts off what lies below the accumulator's last place at each step of 16 inner indices, so sums
 // go in chunks of kNsChunk blocks of 64 indices, the small products of a block first, and the chunks are added in registers (8 x 1024 x 784 fp32, error against 64 bits and
-// time: one block 1.5e-6, 566 us; two 3.1e-6 or more, 550; a plain fp32 chain 2.8e-6); products of one plane each, whose operands are off by 2^-12, take kNsChunkOne, which
-// lets the tensor cores work on the next tile while this one is written (2 x 4096 x 4096 bf16: 3.19 -> 3.10 ms), and those of 16-bit results
-// kNsChunkHalf, off by 5e-6 beside a rounding of 2e-4 or more (3 x 1021 x 2053 fp16: 470 -> 452 us).
-//
-// Results in bf16 (2^-9 an element) of matrices of at least kNsCoarse rows.  An error in a direction is moved on by the later steps, which enlarge it while its singular
-// value is small and keep it (slopes of -1.1 to 1.1 around one) once it is not; in a matrix of many directions, none of which can start out large, that leaves little
-// of the early steps' errors.  With hi hi alone in every step the result is off by 1.9e-3 to 2.8e-3 of its norm (512 rows; rounding to bf16: 1.7e-3), with all products
-// in the square and the last product of the last step but one, and hi hi elsewhere, by 1.1e-3, for 26 instead of 60 products of planes of a square matrix
-// (2 x 4096 x 4096: 7.6 -> 3.5 ms).  A direction that holds most of the norm from the start can be off by 2e-2 of itself, so smaller matrices, where
-// many can (64 rows: 2.3e-3 in all), take all products.
+// time: one block 1.5e-6, 566 us; two 3.1e-6 or more, 550; a plain fp32 chain 2.8e-6).
+// The type that the result is stored in changes nothing of that: what an error grows to depends on how the norm of G is spread over its directions, on the
+// coefficients and on the steps.  With hi hi alone in most places (2 x 4096 x 4096 bf16 in 3.2 instead of 7.2 ms) a dense result of 512 rows was off by 1.2e-3 of its norm after
+// five steps (rounding to bf16: 1.7e-3), but one of eight rows that hold all of the norm by 8e-3, and with (4.0848, -6.8946, 2.9270) by 6e-2; with 512 indices in an
+// accumulator (6.3 ms) a dense fp16 result was off by about 1e-4 after ten steps (rounding: 2e-4; this form and the fp32 chain: 1e-5).
 #pragma once
 
 #include <algorithm>
@@ -180,23 +175,21 @@ constexpr int kNsThreads = 384;  // warp 0: TMA, warp 1: MMA and tensor memory, 
 constexpr int kNsRegsIssue = 56, kNsRegsDrain = 216;
 static_assert((kNsRegsIssue + 2 * kNsRegsDrain) * 128 <= 168 * kNsThreads, "setmaxnreg draws on the registers of the launch");
 constexpr int kNsK = 64;
-constexpr int kNsChunk = 1, kNsChunkHalf = 8, kNsChunkOne = 64, kNsCoarse = 512;
+constexpr int kNsChunk = 1;  // blocks of 64 inner indices that share an accumulator
 constexpr int kNsMaxStages = 8, kNsRing = 192 * 1024, kNsSmem = kNsRing + 8 * 4096 + 1024 + 256;
 
 enum : int { NS_GRAM = 0, NS_SQUARE = 1, NS_APPLY = 2, NS_FINAL = 3, NS_PART = 4 };  // NS_PART: a share of a Gram matrix's inner indices, in fp32
 
 struct NsGemm {
   int m, n, inner;        // of the product
-  int tile_n, m_tiles, n_tiles, na, nb;  // na, nb: planes of A and B that enter (2: all three products; hi hi alone where both are 1)
-  int chunk;              // blocks of 64 inner indices that share an accumulator
-  int half_result;        // the result is stored in 16 bits
+  int tile_n, m_tiles, n_tiles;
   int stages, stage_bytes, a_bytes, b_bytes;
   uint32_t idesc;
   int sym;                // a symmetric result: tiles below the diagonal are the transposed ones above
   int splits, split_blocks;  // NS_PART: shares of the inner indices, blocks of 64 of a share (else 1 and all)
   int64_t per_k, units;   // tiles of a worker (of a share of one), of all
-  float f, h, diagonal;   // result = f * product + h * (hi + lo of `other`), and `diagonal` on the diagonal of a square one
-  NsPlanes other, out;    // the same sizes; `out`: not NS_FINAL; `other` is not read with h = 0
+  float f, h, diagonal;   // result = f * product; NS_SQUARE: + h * (hi + lo of `other`) + diagonal * I
+  NsPlanes other, out;    // the same sizes; `out`: not NS_FINAL
   void* final_out;        // NS_FINAL
   int64_t ok, oi, oj;
 };
@@ -316,7 +309,7 @@ __device__ __forceinline__ void ns_store_final(const float (&v)[32], const NsGem
 }
 
 // grid: CTAs (PAIR: clusters of 2 that share a tile of 256 rows, cta_group::2), each walking tiles u, u + grid, ...
-// A stage holds 64 inner indices of every plane that enters: [A planes][B planes].  All waits are bounded; a CTA that gives up leaves NaN in its tiles.
+// A stage holds 64 inner indices of every plane: [A hi, lo][B hi, lo].  All waits are bounded; a CTA that gives up leaves NaN in its tiles.
 template <typename T, int EPI, bool PAIR>
 __global__ void __launch_bounds__(kNsThreads, 1)
 ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const NsGemm g) {
@@ -377,7 +370,7 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       bool ok = true;
       const uint32_t ring0 = tc::smem_u32(ring), full0 = tc::smem_u32(full), empty0 = tc::smem_u32(empty);
       const uint32_t bar0 = PAIR ? tc::map_to_cta(full0, 0u) : full0;
-      const uint32_t tx = (PAIR ? 2u : 1u) * (uint32_t)(g.na * g.a_bytes + g.nb * g.b_bytes);
+      const uint32_t tx = (PAIR ? 2u : 1u) * (uint32_t)g.stage_bytes;
       for (int64_t u = unit; u < g.units && ok; u += units) {
         int k, mt, nt;
         ns_tile<SYM, TM>(g, u, k, mt, nt);
@@ -388,8 +381,8 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           const uint32_t bar = bar0 + 8 * s;
           if (!PAIR || one) {
             if (!PAIR || leader) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full0 + 8 * s), "r"(tx) : "memory");
-            for (int p = 0; p < g.na; ++p, dst += g.a_bytes) ht_load<PAIR>(dst, &map_a, kb * kNsK, r0, z + p, bar);
-            for (int p = 0; p < g.nb; ++p, dst += g.b_bytes) {
+            for (int p = 0; p < 2; ++p, dst += g.a_bytes) ht_load<PAIR>(dst, &map_a, kb * kNsK, r0, z + p, bar);
+            for (int p = 0; p < 2; ++p, dst += g.b_bytes) {
               if (B_MN) {
                 for (int i = 0; i < b_rows / 64; ++i) ht_load<PAIR>(dst + i * 8192, &map_b, c0 + 64 * i, kb * kNsK, z + p, bar);
               } else {
@@ -419,18 +412,14 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           }
           if (!ht_wait<LIMIT>(full0 + 8 * s, ph, abort_flag)) { ok = false; break; }
           tc::tc_fence_after();
-          const uint32_t d = tmem_base + (uint32_t)as * acc_cols, a_hi = (ring_lo + s * step) | A_LBO, b_hi = (ring_lo + s * step + g.na * a_pl) | B_LBO;
-          const bool last = in_chunk == g.chunk - 1 || kb == kb1 - 1;
+          const uint32_t d = tmem_base + (uint32_t)as * acc_cols, a_hi = (ring_lo + s * step) | A_LBO, b_hi = (ring_lo + s * step + 2 * a_pl) | B_LBO;
+          const bool last = in_chunk == kNsChunk - 1 || kb == kb1 - 1;
           if (!PAIR || one) {
             uint32_t more = in_chunk;
-            if (g.na == 2) {
 #pragma unroll
-              for (int i = 0; i < kNsK / 16; ++i, more = 1) ht_mma<PAIR>(d, a_hi + a_pl + 2 * i, b_hi + B_STEP * i, g.idesc, more);
-            }
-            if (g.nb == 2) {
+            for (int i = 0; i < kNsK / 16; ++i, more = 1) ht_mma<PAIR>(d, a_hi + a_pl + 2 * i, b_hi + B_STEP * i, g.idesc, more);
 #pragma unroll
-              for (int i = 0; i < kNsK / 16; ++i, more = 1) ht_mma<PAIR>(d, a_hi + 2 * i, b_hi + b_pl + B_STEP * i, g.idesc, more);
-            }
+            for (int i = 0; i < kNsK / 16; ++i, more = 1) ht_mma<PAIR>(d, a_hi + 2 * i, b_hi + b_pl + B_STEP * i, g.idesc, more);
 #pragma unroll
             for (int i = 0; i < kNsK / 16; ++i, more = 1) ht_mma<PAIR>(d, a_hi + 2 * i, b_hi + B_STEP * i, g.idesc, more);
             ht_commit<PAIR>(empty0 + 8 * s);
@@ -456,7 +445,7 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     for (int64_t u = unit; u < g.units; u += units) {
       int k, mt, nt;
       ns_tile<SYM, TM>(g, u, k, mt, nt);
-      const int chunks = (end_block(k) - first_block(k) + g.chunk - 1) / g.chunk;
+      const int chunks = (end_block(k) - first_block(k) + kNsChunk - 1) / kNsChunk;
       const int64_t i = (int64_t)mt * TM + (int64_t)rank * 128 + quad * 32 + lane;
       const int64_t c_tile = (int64_t)nt * g.tile_n;
       const int nv = (int)min((int64_t)g.tile_n, g.n - c_tile);
@@ -511,7 +500,7 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           for (int j = 0; j < 32; ++j) v[j] = NAN;
         }
         if (!WHOLE) ns_stage_free(lane);
-        if (EPI != NS_GRAM && EPI != NS_PART && g.h != 0.f) ns_add_planes(v, g.h, g.other.p + (int64_t)k * 2 * g.other.plane, g.other.plane, g.other.ld, i0, g.m, c, stage, lane);
+        if (EPI == NS_SQUARE && g.h != 0.f) ns_add_planes(v, g.h, g.other.p + (int64_t)k * 2 * g.other.plane, g.other.plane, g.other.ld, i0, g.m, c, stage, lane);
         if (WHOLE) {
           ns_store_final<T>(v, g, k, i0, c, reinterpret_cast<float*>(stage), lane);
         } else {
@@ -572,9 +561,8 @@ inline void ns_plan(NsGemm& g, int32_t K, bool sym, bool b_mn) {
   g.units = g.per_k * K * g.splits;
   g.a_bytes = 128 * kNsK * 2;
   g.b_bytes = (pair ? g.tile_n / 2 : g.tile_n) * kNsK * 2;
-  g.stage_bytes = g.na * g.a_bytes + g.nb * g.b_bytes;
+  g.stage_bytes = 2 * (g.a_bytes + g.b_bytes);
   g.stages = std::min(kNsMaxStages, kNsRing / g.stage_bytes);
-  g.chunk = g.na + g.nb == 2 ? kNsChunkOne : g.half_result ? kNsChunkHalf : kNsChunk;
   g.idesc = tc::instr_desc(tm, g.tile_n, false, b_mn) & ~((1u << 7) | (1u << 10));  // operands f16
 }
 
