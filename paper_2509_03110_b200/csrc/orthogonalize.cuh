@@ -70,7 +70,9 @@ ns_norm_kernel(const T* g, int64_t sk, int64_t so, int64_t si, int64_t inner, in
   s = block_sum(s, smem);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
-// 1 / (|G| + eps), in every thread of a block of 256: the partial sums in a fixed order
+// 1 / (|G| + eps) of |G|^2 = s; NaN, not 0, where an element is infinite
+__device__ inline double ns_inverse_of(double s, double eps) { return isinf(s) ? (double)NAN : 1.0 / (sqrt(s) + eps); }
+// The same of partial sums, in a fixed order, in every thread of a block of 256
 __device__ inline double ns_inverse(const double* part, int chunks, float eps) {
   __shared__ double smem[9];
   double s = 0.0;
@@ -78,7 +80,7 @@ __device__ inline double ns_inverse(const double* part, int chunks, float eps) {
   s = block_sum(s, smem);
   if (threadIdx.x == 0) smem[8] = s;
   __syncthreads();
-  return 1.0 / (sqrt(smem[8]) + (double)eps);
+  return ns_inverse_of(smem[8], (double)eps);
 }
 
 __device__ inline void ns_split(float v, fp16& hi, fp16& lo) {
@@ -745,7 +747,7 @@ ns_small_kernel(const T* g, int64_t sk, int64_t si, int64_t sj, int m, int64_t n
   __syncthreads();
   double trace = 0.0;
   for (int i = 0; i < m; ++i) trace += A[i * LD + i];
-  const double inv = 1.0 / (sqrt(trace) + eps);
+  const double inv = ns_inverse_of(trace, eps);
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < R; ++u)
