@@ -453,7 +453,7 @@ int lsam_embed_grad(const void* d_dout, int32_t dtype, int32_t K, int64_t rows, 
  *  d_rstd_post, d_rstd_pre: q and r, fp32 [K, rows], nullable; what the gradient needs.
  * The sigmoid's exponential and reciprocal come from the special-function unit (a factor of 1 +- (2^-22 + 3 |gate| 2^-24)).
  * out may be x itself (the same strides); otherwise outputs overlap neither inputs nor one another, and their rows neither overlap nor interleave.
- * eps > 0.  A row whose sum of squares leaves the fp32 range has q or r 0; a NaN or an infinity stays in its row. */
+ * eps > 0.  A row whose sum of squares leaves the fp32 range has q or r 0; a NaN or an infinity stays in its row.  With n = 0 there is no mean, and nothing is written. */
 enum { LSAM_GATE_NONE = 0, LSAM_GATE_COLUMN = 1, LSAM_GATE_ROW = 2, LSAM_GATE_FULL = 3 };
 enum { LSAM_ACT_LINEAR = 0, LSAM_ACT_SIGMOID = 1, LSAM_ACT_TANH = 2 };
 typedef struct {
@@ -478,7 +478,8 @@ int lsam_residual_norm(const lsam_residual* r, const lsam_rows* x, const lsam_ro
  * x (dx), branch, gate and the two weights; each result is nullable and left out where it is.
  *  r: as in the forward call (eps is not used); out: what it returned (without a branch: x; not read with pre = 0), d_rstd_post and d_rstd_pre as well.
  *  dx, dbranch and dgate of LSAM_GATE_FULL: rows of `dtype`, strides of their own.  The gradients of fp32 inputs are fp32 and dense: dgate->d [K, n] or,
- *  of a shared gate, [n], summed over the workers (COLUMN), [K, rows] (ROW); d_dpost_weight and d_dpre_weight [K, n] or [n] likewise.  Sums over rows have a fixed order.
+ *  of a shared gate, [n], summed over the workers (COLUMN), [K, rows] (ROW); d_dpost_weight and d_dpre_weight [K, n] or [n] likewise.  Sums over rows have a fixed order;
+ *  sums over no rows, and with n = 0 those of LSAM_GATE_ROW over no columns, are zeros.
  *  Results overlap neither inputs nor one another, except that dx may be dout itself (the same strides).
  *  d_workspace: lsam_residual_norm_grad_workspace_bytes() bytes. */
 size_t lsam_residual_norm_grad_workspace_bytes(int32_t dtype, int32_t K, int64_t rows, int64_t n);

@@ -645,6 +645,10 @@ def lsam_residual_norm(x, branch=None, gate=None, post_weight=None, pre_weight=N
         s = _proto(dev).new_empty(x.shape[:-1]) if q is None else torch.empty_like(q)
         ps = s.data_ptr()
     _call(lib().lsam_residual_norm, r, rx, ro, ru, pq, ps, _raw_stream(dev))
+    if r.n == 0:  # the mean of nothing, which the call leaves unwritten
+        for t in (q, s):
+            if t is not None:
+                t.fill_(float("nan"))
     return tuple.__new__(ResidualNorm, (out, u, q, s))  # without the check of a named tuple's arguments
 
 

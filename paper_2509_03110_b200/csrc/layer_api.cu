@@ -371,7 +371,13 @@ extern "C" int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* 
   if (oz.d && r->gate == LSAM_GATE_NONE) return err.fail(LSAM_ERR_INVALID, "dgate without a gate");
   if (d_dpost_weight && !r->post) return err.fail(LSAM_ERR_INVALID, "d_dpost_weight without post");
   if (d_dpre_weight && !r->pre) return err.fail(LSAM_ERR_INVALID, "d_dpre_weight without pre");
-  if (r->n == 0) return LSAM_OK;
+  if (r->n == 0) {  // rows of no columns: sums over them are zeros
+    if (r->gate != LSAM_GATE_ROW || !oz.d || r->K == 0 || r->rows == 0) return LSAM_OK;
+    PtrCheck pc;
+    pc.need(oz.d, 4);
+    if (pc.why) return err.fail(LSAM_ERR_INVALID, pc.why);
+    return err.done(cudaMemsetAsync(oz.d, 0, (size_t)4 * r->K * r->rows, reinterpret_cast<cudaStream_t>(cuda_stream)));
+  }
   // without dnormed the norm in front of the next block has no part in the gradient
   const bool pre = r->pre && gu.d;
   ResidualCheck ck(*r);
