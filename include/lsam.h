@@ -487,6 +487,13 @@ int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* out, const 
                             const lsam_rows* dx, const lsam_rows* dbranch, const lsam_rows* dgate, float* d_dpost_weight, float* d_dpre_weight, void* d_workspace,
                             size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len);
 
+/* Self-test: lsam_residual_norm_grad of fp32 rows of 4097 to 32768 columns, which a cluster of blocks shares.  In the third row of every block's share of the rows the sums of the last
+ * block never reach the first one, and waits are short: what depends on the sums of that row in the first block's columns, and of the rows behind it in all of them, comes back as NaN,
+ * the rest as from the call itself. */
+int lsam_selftest_residual_wait(const lsam_residual* r, const lsam_rows* out, const float* d_rstd_post, const float* d_rstd_pre, const lsam_rows* dout, const lsam_rows* dnormed,
+                                const lsam_rows* dx, const lsam_rows* dbranch, const lsam_rows* dgate, float* d_dpost_weight, float* d_dpre_weight, void* d_workspace,
+                                size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len);
+
 /* A matrix update made nearly orthogonal:  X_0 = G / (|G|_F + eps),  X_{t+1} = a X_t + (b A + c A^2) X_t with A = X_t X_t^T,  out = scale X_steps:
  * an odd polynomial of the singular values, applied `steps` times, that moves all of them towards one and keeps the singular vectors.  With
  * (a, b, c) = (3.4445, -4.7750, 2.0315) and 5 steps, those of the Muon optimiser, singular values from 0.003 |G|_F up end between 0.68 and 1.21.

@@ -31,7 +31,7 @@ EXPORTS = [
     "lsam_checkpoint_bytes", "lsam_save_checkpoint", "lsam_load_checkpoint", "lsam_read_anchor_gap",
     "lsam_logprob", "lsam_logprob_grad", "lsam_logprob_wide", "lsam_logprob_grad_wide", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout", "lsam_score_batch", "lsam_selftest_head_wait",
     "lsam_embed", "lsam_embed_grad", "lsam_embed_grad_workspace_bytes",
-    "lsam_residual_norm", "lsam_residual_norm_grad", "lsam_residual_norm_grad_workspace_bytes",
+    "lsam_residual_norm", "lsam_residual_norm_grad", "lsam_residual_norm_grad_workspace_bytes", "lsam_selftest_residual_wait",
     "lsam_orthogonalize", "lsam_orthogonalize_workspace_bytes",
 ]
 
@@ -143,7 +143,8 @@ def lib():
     L.lsam_residual_norm.argtypes = [xp, rp, rp, rp, vp, vp] + err
     L.lsam_residual_norm_grad_workspace_bytes.restype = C.c_size_t
     L.lsam_residual_norm_grad_workspace_bytes.argtypes = [i32, i32, i64, i64]
-    L.lsam_residual_norm_grad.argtypes = [xp, rp, vp, vp] + [rp] * 5 + [vp, vp, vp, C.c_size_t] + err
+    for fn in (L.lsam_residual_norm_grad, L.lsam_selftest_residual_wait):
+        fn.argtypes = [xp, rp, vp, vp] + [rp] * 5 + [vp, vp, vp, C.c_size_t] + err
     f32 = C.c_float
     L.lsam_orthogonalize_workspace_bytes.restype = C.c_size_t
     L.lsam_orthogonalize_workspace_bytes.argtypes = [i32, i32, i64, i64]

@@ -358,10 +358,11 @@ extern "C" size_t lsam_residual_norm_grad_workspace_bytes(int32_t dtype, int32_t
   return norm_grad_plan(dtype, K, rows, n).total;
 }
 
-extern "C" int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* out, const float* d_rstd_post, const float* d_rstd_pre, const lsam_rows* dout, const lsam_rows* dnormed,
-                                       const lsam_rows* dx, const lsam_rows* dbranch, const lsam_rows* dgate, float* d_dpost_weight, float* d_dpre_weight, void* d_workspace,
-                                       size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len) {
-  const Err err("lsam_residual_norm_grad", h_err, h_err_len);
+namespace {
+
+int residual_norm_grad(const Err& err, const lsam_residual* r, const lsam_rows* out, const float* d_rstd_post, const float* d_rstd_pre, const lsam_rows* dout, const lsam_rows* dnormed,
+                       const lsam_rows* dx, const lsam_rows* dbranch, const lsam_rows* dgate, float* d_dpost_weight, float* d_dpre_weight, void* d_workspace, size_t workspace_bytes,
+                       bool starved, void* cuda_stream) {
   if (!r) return err.fail(LSAM_ERR_INVALID, "a required pointer is NULL");
   if (const char* why = residual_why(*r)) return err.fail(LSAM_ERR_INVALID, why);
   const lsam_rows y = out ? *out : kNoRows, gy = dout ? *dout : kNoRows, gu = dnormed ? *dnormed : kNoRows, ox = dx ? *dx : kNoRows, ob = dbranch ? *dbranch : kNoRows,
@@ -398,6 +399,7 @@ extern "C" int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* 
   NormGradPlan p{};
   if (!empty) {
     p = norm_grad_plan(r->dtype, r->K, r->rows, r->n);
+    if (starved && (r->dtype != LSAM_FP32 || p.ranks < 2)) return err.fail(LSAM_ERR_INVALID, "these rows are not shared by a cluster of blocks, or not fp32");
     if (workspace_bytes < p.total) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_residual_norm_grad_workspace_bytes()");
     if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return err.fail(LSAM_ERR_WORKSPACE, "workspace not 256-byte aligned");
     ck.pc.need(d_workspace, 256);
@@ -436,6 +438,12 @@ extern "C" int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* 
           cfg.gridDim = dim3((unsigned)(p.blocks * p.ranks)); cfg.blockDim = dim3(std::max(128, p.threads)); cfg.stream = stream; cfg.attrs = attr; cfg.numAttrs = p.ranks > 1 ? 1 : 0;
           return cudaLaunchKernelEx(&cfg, kern, a);
         };
+        if constexpr (std::is_same<T, float>::value) {
+          if (starved) {
+            e = vec ? go(residual_norm_grad_fused_kernel<T, 512, true, true, FORM_ANY, true>) : go(residual_norm_grad_fused_kernel<T, 512, false, true, FORM_ANY, true>);
+            return;
+          }
+        }
         const auto pick = [&](auto v, auto f) {
           constexpr bool V = decltype(v)::value;
           constexpr int F = decltype(f)::value;
@@ -466,6 +474,22 @@ extern "C" int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* 
     e = launch_behind(residual_norm_grad_sum_kernel, grid, dim3(32, kNormSumLanes), 0, stream, sum);
   }
   return err.done(e);
+}
+
+}  // namespace
+
+extern "C" int lsam_residual_norm_grad(const lsam_residual* r, const lsam_rows* out, const float* d_rstd_post, const float* d_rstd_pre, const lsam_rows* dout, const lsam_rows* dnormed,
+                                       const lsam_rows* dx, const lsam_rows* dbranch, const lsam_rows* dgate, float* d_dpost_weight, float* d_dpre_weight, void* d_workspace,
+                                       size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len) {
+  return residual_norm_grad(Err("lsam_residual_norm_grad", h_err, h_err_len), r, out, d_rstd_post, d_rstd_pre, dout, dnormed, dx, dbranch, dgate, d_dpost_weight, d_dpre_weight, d_workspace,
+                            workspace_bytes, false, cuda_stream);
+}
+
+extern "C" int lsam_selftest_residual_wait(const lsam_residual* r, const lsam_rows* out, const float* d_rstd_post, const float* d_rstd_pre, const lsam_rows* dout, const lsam_rows* dnormed,
+                                           const lsam_rows* dx, const lsam_rows* dbranch, const lsam_rows* dgate, float* d_dpost_weight, float* d_dpre_weight, void* d_workspace,
+                                           size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len) {
+  return residual_norm_grad(Err("lsam_selftest_residual_wait", h_err, h_err_len), r, out, d_rstd_post, d_rstd_pre, dout, dnormed, dx, dbranch, dgate, d_dpost_weight, d_dpre_weight,
+                            d_workspace, workspace_bytes, true, cuda_stream);
 }
 
 // ------------------------------------------------------------------------------------------------ orthogonalisation

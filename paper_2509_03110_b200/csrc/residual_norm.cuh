@@ -379,7 +379,8 @@ constexpr int kGradRanks = 8;  // blocks of a cluster, at most
 // a test of what is there.
 // TURNS: rows that a block works on at a time.  Rows of more than 4096 columns are shared by a cluster of blocks, `per` columns each (CLUSTER), which send
 // their sums to one another.
-template <typename T, int NT, bool VEC, bool CLUSTER, int FORM>
+// STARVED (self-test): the sums of the last block never reach the first one in the third row of every strip, and waits are short.
+template <typename T, int NT, bool VEC, bool CLUSTER, int FORM, bool STARVED = false>
 __global__ void __launch_bounds__(norm_threads(NT), 512 / norm_threads(NT))
 residual_norm_grad_fused_kernel(NormGradArgs<T> a) {
   constexpr int E = 8, P = E / 2, TURNS = NT == 32 ? 4 : 1, WARPS = NT / 32, RANKS = CLUSTER ? kGradRanks : 1;
@@ -402,7 +403,8 @@ residual_norm_grad_fused_kernel(NormGradArgs<T> a) {
   }
   // Sums travel as asynchronous stores that count on the receiver's barrier: a barrier of the cluster, whose release waits for every global store before it, took
   // 1.5 us a row.  Nobody can send for the row after next before every warp has sent for the next one, so two sets of sums are enough.  The wait is
-  // bounded; a block whose wait runs out goes on with NaN.
+  // bounded.  A thread whose wait runs out goes on with NaN and neither sends nor waits again: whatever it sent would land, too early, in a set that another
+  // block may still read.  So the others' next row stays incomplete, their waits run out in turn, and no row is made of a mixture.
   __shared__ uint64_t arrived[2];
   __shared__ volatile int never;
   uint32_t phase = 0;
@@ -518,11 +520,11 @@ residual_norm_grad_fused_kernel(NormGradArgs<T> a) {
         x += __shfl_xor_sync(~0u, x, 4);
         x += __shfl_xor_sync(~0u, x, 2);
         x += __shfl_xor_sync(~0u, x, 1);
-        if ((lane & 7) == 0 && lane < 24) {
+        if ((lane & 7) == 0 && lane < 24 && !dead) {
           float* to = &sums[parity][CLUSTER ? rank : 0][lane >> 3][threadIdx.x >> 5];
           if constexpr (CLUSTER) {
             const uint32_t at = tc::smem_u32(to), bar = tc::smem_u32(&arrived[parity]);
-            for (uint32_t c = 0; c < ranks; ++c)
+            for (uint32_t c = STARVED && rank == ranks - 1 && i == first + 2 ? 1u : 0u; c < ranks; ++c)
               asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(tc::map_to_cta(at, c)), "f"(x), "r"(tc::map_to_cta(bar, c)) : "memory");
           } else {
             *to = x;
@@ -530,8 +532,10 @@ residual_norm_grad_fused_kernel(NormGradArgs<T> a) {
         }
         // the other half was read before it
         if constexpr (CLUSTER) {
-          if (threadIdx.x == 0) tc::mbar_expect_tx(&arrived[parity], ranks * WARPS * 12);
-          if (!dead && !tc::mbar_wait_limit(&arrived[parity], phase, &never, tc::kSpinLimit)) dead = 1;
+          if (!dead) {
+            if (threadIdx.x == 0) tc::mbar_expect_tx(&arrived[parity], ranks * WARPS * 12);
+            if (!tc::mbar_wait_limit(&arrived[parity], phase, &never, STARVED ? 1u << 13 : tc::kSpinLimit)) dead = 1;
+          }
           if (parity) phase ^= 1u;
         } else {
           __syncthreads();
@@ -599,8 +603,14 @@ residual_norm_grad_fused_kernel(NormGradArgs<T> a) {
     base += a.rows;
     ++k;
   }
-  // no block leaves while another's sums may still be on their way to it
-  if constexpr (CLUSTER) tc::cluster_sync_all();
+  // no block leaves while another's sums may still be on their way to it: all have sent what they will, and what a block has not waited for gets a millisecond to land
+  if constexpr (CLUSTER) {
+    tc::cluster_sync_all();
+    if (dead) {
+      const long long t0 = clock64();
+      while (clock64() - t0 < 2000000LL) { }
+    }
+  }
 }
 
 // Rows of more columns than a cluster holds: two passes.
