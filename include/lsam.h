@@ -510,6 +510,12 @@ int lsam_orthogonalize(const void* d_g, int32_t dtype, int32_t K, int64_t rows, 
                        float b, float c, float scale, float eps, void* d_out, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_col, void* d_workspace,
                        size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len);
 
+/* Self-test: lsam_orthogonalize of fp32 matrices of more than 32 rows and columns with at least one step, none of whose products' operands is ever copied: every wait for one runs out after a
+ * short limit, and the whole result comes back as NaN. */
+int lsam_selftest_orthogonalize_wait(const void* d_g, int32_t dtype, int32_t K, int64_t rows, int64_t cols, int64_t stride_k, int64_t stride_row, int64_t stride_col, int32_t steps,
+                                     float a, float b, float c, float scale, float eps, void* d_out, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_col,
+                                     void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,7 +32,7 @@ EXPORTS = [
     "lsam_logprob", "lsam_logprob_grad", "lsam_logprob_wide", "lsam_logprob_grad_wide", "lsam_head_logprob", "lsam_head_logprob_workspace_bytes", "lsam_dropout", "lsam_score_batch", "lsam_selftest_head_wait",
     "lsam_embed", "lsam_embed_grad", "lsam_embed_grad_workspace_bytes",
     "lsam_residual_norm", "lsam_residual_norm_grad", "lsam_residual_norm_grad_workspace_bytes", "lsam_selftest_residual_wait",
-    "lsam_orthogonalize", "lsam_orthogonalize_workspace_bytes",
+    "lsam_orthogonalize", "lsam_orthogonalize_workspace_bytes", "lsam_selftest_orthogonalize_wait",
 ]
 
 
@@ -148,7 +148,8 @@ def lib():
     f32 = C.c_float
     L.lsam_orthogonalize_workspace_bytes.restype = C.c_size_t
     L.lsam_orthogonalize_workspace_bytes.argtypes = [i32, i32, i64, i64]
-    L.lsam_orthogonalize.argtypes = [vp, i32, i32] + [i64] * 5 + [i32] + [f32] * 5 + [vp] + [i64] * 3 + [vp, C.c_size_t] + err
+    for fn in (L.lsam_orthogonalize, L.lsam_selftest_orthogonalize_wait):
+        fn.argtypes = [vp, i32, i32] + [i64] * 5 + [i32] + [f32] * 5 + [vp] + [i64] * 3 + [vp, C.c_size_t] + err
     _lib = L
     return L
 

@@ -565,10 +565,11 @@ extern "C" size_t lsam_orthogonalize_workspace_bytes(int32_t dtype, int32_t K, i
   return ortho_plan(K, rows, cols).total;
 }
 
-extern "C" int lsam_orthogonalize(const void* d_g, int32_t dtype, int32_t K, int64_t rows, int64_t cols, int64_t stride_k, int64_t stride_row, int64_t stride_col, int32_t steps, float a,
-                                  float b, float c, float scale, float eps, void* d_out, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_col, void* d_workspace,
-                                  size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len) {
-  const Err err("lsam_orthogonalize", h_err, h_err_len);
+namespace {
+
+int orthogonalize(const Err& err, const void* d_g, int32_t dtype, int32_t K, int64_t rows, int64_t cols, int64_t stride_k, int64_t stride_row, int64_t stride_col, int32_t steps, float a, float b,
+                  float c, float scale, float eps, void* d_out, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_col, void* d_workspace, size_t workspace_bytes, bool starved,
+                  void* cuda_stream) {
   if (!dtype_ok(dtype)) return err.fail(LSAM_ERR_INVALID, "unknown dtype");
   if (K < 0 || rows < 0 || cols < 0 || K > 65535 || rows > kMaxSide || cols > kMaxSide) return err.fail(LSAM_ERR_INVALID, "need 0 <= K <= 65535 and 0 <= rows, cols <= 2^20");
   if (steps < 0 || steps > 32) return err.fail(LSAM_ERR_INVALID, "steps outside 0 .. 32");
@@ -587,6 +588,7 @@ extern "C" int lsam_orthogonalize(const void* d_g, int32_t dtype, int32_t K, int
     return err.fail(LSAM_ERR_INVALID, "a stride is negative or a tensor is too large");
   if (!disjoint(K, out_stride_k, rows, out_stride_row, cols, out_stride_col)) return err.fail(LSAM_ERR_INVALID, "elements of the output share an address or interleave");
   const OrthoPlan q = ortho_plan(K, rows, cols);
+  if (starved && (dtype != LSAM_FP32 || q.m <= kNsSmall || steps == 0)) return err.fail(LSAM_ERR_INVALID, "these matrices do not go to the tensor cores, or are not fp32");
   if (workspace_bytes < q.total) return err.fail(LSAM_ERR_WORKSPACE, "workspace smaller than lsam_orthogonalize_workspace_bytes()");
   if (q.total && reinterpret_cast<uintptr_t>(d_workspace) & 255) return err.fail(LSAM_ERR_WORKSPACE, "workspace not 256-byte aligned");
   const size_t es = dtype_size(dtype);
@@ -662,32 +664,48 @@ extern "C" int lsam_orthogonalize(const void* d_g, int32_t dtype, int32_t K, int
         v.f = 1.f;
         float* sums = reinterpret_cast<float*>(ws + q.part);
         v.final_out = sums; v.ok = m * q.ldm; v.oi = q.ldm; v.oj = 1;
-        e = ns_launch<float, NS_PART>(x, x, v, K, stream);
+        e = ns_launch<float, NS_PART>(x, x, v, K, starved, stream);
         if (e == cudaSuccess)
           e = launch_behind(ns_join_kernel, dim3((unsigned)ceil_div(m * q.ldm, 1024), (unsigned)K), dim3(256), 0, stream, static_cast<const float*>(sums), q.splits, m, A, w.f);
       } else {
-        e = ns_launch<fp16, NS_GRAM>(x, x, w, K, stream);
+        e = ns_launch<fp16, NS_GRAM>(x, x, w, K, starved, stream);
       }
       if (e != cudaSuccess) return;
       w.inner = (int)m;
       // the term a X of the last product is the diagonal of P
       w.f = c * two(ep - 2 * ea); w.h = b * two(ep - ea); w.diagonal = a * two(ep);
       w.other = A; w.out = P;
-      e = ns_launch<fp16, NS_SQUARE>(A, A, w, K, stream);
+      e = ns_launch<fp16, NS_SQUARE>(A, A, w, K, starved, stream);
       if (e != cudaSuccess) return;
       w.n = (int)n;
       w.out = y;
       if (s + 1 < steps) {
         w.f = two(en - ep - ex);
-        e = ns_launch<fp16, NS_APPLY>(P, x, w, K, stream);
+        e = ns_launch<fp16, NS_APPLY>(P, x, w, K, starved, stream);
       } else {
         w.f = scale * two(-ep - ex);
         w.final_out = out; w.ok = out_stride_k; w.oi = oi; w.oj = oj;
-        e = ns_launch<T, NS_FINAL>(P, x, w, K, stream);
+        e = ns_launch<T, NS_FINAL>(P, x, w, K, starved, stream);
       }
       std::swap(x, y);
       top = next; ex = en;
     }
   });
   return err.done(e);
+}
+
+}  // namespace
+
+extern "C" int lsam_orthogonalize(const void* d_g, int32_t dtype, int32_t K, int64_t rows, int64_t cols, int64_t stride_k, int64_t stride_row, int64_t stride_col, int32_t steps, float a,
+                                  float b, float c, float scale, float eps, void* d_out, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_col, void* d_workspace,
+                                  size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len) {
+  return orthogonalize(Err("lsam_orthogonalize", h_err, h_err_len), d_g, dtype, K, rows, cols, stride_k, stride_row, stride_col, steps, a, b, c, scale, eps, d_out, out_stride_k, out_stride_row,
+                       out_stride_col, d_workspace, workspace_bytes, false, cuda_stream);
+}
+
+extern "C" int lsam_selftest_orthogonalize_wait(const void* d_g, int32_t dtype, int32_t K, int64_t rows, int64_t cols, int64_t stride_k, int64_t stride_row, int64_t stride_col, int32_t steps,
+                                                float a, float b, float c, float scale, float eps, void* d_out, int64_t out_stride_k, int64_t out_stride_row, int64_t out_stride_col,
+                                                void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* h_err, size_t h_err_len) {
+  return orthogonalize(Err("lsam_selftest_orthogonalize_wait", h_err, h_err_len), d_g, dtype, K, rows, cols, stride_k, stride_row, stride_col, steps, a, b, c, scale, eps, d_out, out_stride_k,
+                       out_stride_row, out_stride_col, d_workspace, workspace_bytes, true, cuda_stream);
 }

@@ -312,12 +312,13 @@ __device__ __forceinline__ void ns_store_final(const float (&v)[32], const NsGem
 
 // grid: CTAs (PAIR: clusters of 2 that share a tile of 256 rows, cta_group::2), each walking tiles u, u + grid, ...
 // A stage holds 64 inner indices of every plane: [A hi, lo][B hi, lo].  All waits are bounded; a CTA that gives up leaves NaN in its tiles.
-template <typename T, int EPI, bool PAIR>
+// STARVED (self-test): no operand is ever copied and the waits are short, so all of them run out with nothing in flight.
+template <typename T, int EPI, bool PAIR, bool STARVED>
 __global__ void __launch_bounds__(kNsThreads, 1)
 ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const NsGemm g) {
   constexpr bool SYM = EPI == NS_GRAM || EPI == NS_SQUARE, B_MN = EPI == NS_APPLY || EPI == NS_FINAL, WHOLE = EPI == NS_FINAL || EPI == NS_PART;  // WHOLE: no planes
   constexpr int TM = PAIR ? 256 : 128;
-  constexpr uint32_t LIMIT = tc::kSpinLimit;
+  constexpr uint32_t LIMIT = STARVED ? 1u << 13 : tc::kSpinLimit;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* stages = ring + kNsRing;  // [8 draining warps][4 KB]
@@ -366,7 +367,7 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kNsRegsIssue));
     const bool one = ht_elect();
-    if (warp == 0 && (PAIR || one)) {
+    if (!STARVED && warp == 0 && (PAIR || one)) {
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
@@ -598,7 +599,7 @@ ns_join_kernel(const float* part, int splits, int64_t m, NsPlanes out, float f) 
 }
 
 template <typename T, int EPI>
-inline cudaError_t ns_launch(const NsPlanes& A, const NsPlanes& B, NsGemm g, int32_t K, cudaStream_t stream) {
+inline cudaError_t ns_launch(const NsPlanes& A, const NsPlanes& B, NsGemm g, int32_t K, bool starved, cudaStream_t stream) {
   constexpr bool b_mn = EPI == NS_APPLY || EPI == NS_FINAL;
   if (EPI != NS_PART) { g.splits = 1; g.split_blocks = 0; }
   ns_plan(g, K, EPI == NS_GRAM || EPI == NS_SQUARE, b_mn);
@@ -608,7 +609,10 @@ inline cudaError_t ns_launch(const NsPlanes& A, const NsPlanes& B, NsGemm g, int
   if (EPI == NS_FINAL || EPI == NS_PART) mo = ma;
   else if (!ns_make_map(&mo, g.out, g.m, g.n, K, 32, 32)) return cudaErrorInvalidValue;
   if (!(b_mn ? ns_make_map(&mb, B, g.inner, g.n, K, 64) : ns_make_map(&mb, B, g.n, g.inner, K, (uint32_t)(pair ? g.tile_n / 2 : g.tile_n)))) return cudaErrorInvalidValue;
-  const void* kern = pair ? (const void*)ns_gemm_kernel<T, EPI, true> : (const void*)ns_gemm_kernel<T, EPI, false>;
+  const void* kern = pair ? (const void*)ns_gemm_kernel<T, EPI, true, false> : (const void*)ns_gemm_kernel<T, EPI, false, false>;
+  if constexpr (EPI != NS_FINAL || std::is_same<T, float>::value) {  // the self-test is of fp32 results
+    if (starved) kern = pair ? (const void*)ns_gemm_kernel<T, EPI, true, true> : (const void*)ns_gemm_kernel<T, EPI, false, true>;
+  }
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kNsSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};

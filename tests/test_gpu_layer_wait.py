@@ -51,3 +51,21 @@ def test_sums_of_a_cluster_that_never_arrive(rows, n):
     assert torch.isnan(got[3]).all() and torch.equal(got[4], want[4])
     again = G.lsam_residual_norm_grad(fwd, dy, du, act="sigmoid", **how)
     assert all(torch.equal(a, w) for a, w in zip(again, want))
+
+
+# one CTA a tile, pairs, symmetric tiles with and without transposed ones, tall matrices, a Gram matrix that is shared out, several tiles a CTA
+@pytest.mark.parametrize("K, rows, cols, steps", [(2, 40, 70, 1), (1, 128, 130, 2), (2, 300, 520, 2), (1, 777, 300, 1), (1, 128, 4096, 2), (3, 1100, 1100, 1), (40, 200, 210, 1)])
+def test_operands_that_never_arrive(K, rows, cols, steps):
+    g = torch.randn((K, rows, cols), generator=torch.Generator(device="cuda").manual_seed(cols), device="cuda")
+    want, got = G.lsam_orthogonalize(g), torch.full_like(g, 5.0)
+    nbytes = G.lib().lsam_orthogonalize_workspace_bytes(G.FP32, K, rows, cols)
+    ws, at = scratch(nbytes)
+    err = C.create_string_buffer(256)
+    torch.cuda.synchronize()
+    size = rows * cols
+    rc = G.lib().lsam_selftest_orthogonalize_wait(g.data_ptr(), G.FP32, K, rows, cols, size, cols, 1, steps, 3.4445, -4.775, 2.0315, 1.0, 1e-7, got.data_ptr(), size, cols, 1, at, nbytes,
+                                                  torch.cuda.current_stream().cuda_stream, err, 256)
+    assert rc == G.LSAM_OK, err.value
+    torch.cuda.synchronize()
+    assert torch.isnan(got).all()
+    assert torch.equal(G.lsam_orthogonalize(g), want)
