@@ -454,7 +454,8 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       const int nv = (int)min((int64_t)g.tile_n, g.n - c_tile);
       float l[4][32];  // this warp's blocks of 32 columns: half, half + 2, ...
       for (int ch = 0; ch < chunks && ok; ++ch) {
-        if (!tc::mbar_wait_limit(&acc_full[as], aph, abort_flag, LIMIT)) { ok = false; break; }
+        // as a warp: what follows is for all of its lanes, or for none
+        if (!__all_sync(~0u, tc::mbar_wait_limit(&acc_full[as], aph, abort_flag, LIMIT))) { ok = false; break; }
         tc::tc_fence_after();
         const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)as * acc_cols;
         if (ch == 0) {
