@@ -451,7 +451,8 @@ int lsam_embed_grad(const void* d_dout, int32_t dtype, int32_t K, int64_t rows, 
  *  branch, gate (LSAM_GATE_FULL), x, out, normed: [K, rows, n] of `dtype`, columns contiguous.  d_gate otherwise: LSAM_GATE_COLUMN fp32 [K, n] (stride_k 0:
  *  shared), LSAM_GATE_ROW fp32 [K, rows], dense.  d_post_weight, d_pre_weight: fp32 [K, n] (stride 0: shared) or NULL (1).
  *  d_rstd_post, d_rstd_pre: q and r, fp32 [K, rows], nullable; what the gradient needs.
- * The sigmoid's exponential and reciprocal come from the special-function unit (a factor of 1 +- (2^-22 + 3 |gate| 2^-24)).
+ * The sigmoid's exponential and reciprocal come from the special-function unit (a factor of 1 +- (2^-22 + 3 |gate| 2^-24); values below 2^-126 are 0).  In the gradient the
+ * slope is made of the value v, as v (1 - v) or 1 - v^2: off by 2^-21 at most, which is much of the slope itself where a gate is saturated.
  * out may be x itself (the same strides); otherwise outputs overlap neither inputs nor one another, and their rows neither overlap nor interleave.
  * eps > 0.  A row whose sum of squares leaves the fp32 range has q or r 0; a NaN or an infinity stays in its row.  With n = 0 there is no mean, and nothing is written. */
 enum { LSAM_GATE_NONE = 0, LSAM_GATE_COLUMN = 1, LSAM_GATE_ROW = 2, LSAM_GATE_FULL = 3 };
@@ -501,7 +502,7 @@ int lsam_selftest_residual_wait(const lsam_residual* r, const lsam_rows* out, co
  *  else it must not overlap it.  One matrix per worker, each normed by itself; a matrix of zeros stays zero (eps > 0).
  * Products of fp32 accuracy whatever the type (two fp16 planes of every matrix, three products of planes, fp32 sums); an element of X_t is held to 2^-24 of itself or 2^-38 of the
  * largest singular value that the coefficients allow at that step, whichever is more.  Up to 32 rows or columns: in double throughout.  The steps carry errors on as they do in a chain of plain fp32
- * products (with the coefficients above: 1e-6 to 1e-5 of the result's norm); coefficients that do not let singular values settle enlarge them at every step.  A NaN or an infinity in a matrix makes all of it NaN, and so does a matrix of zeros with eps = 0.
+ * products (with the coefficients above and 5 to 10 steps: 1e-6 to 1e-5 of the result's norm); coefficients that do not let singular values settle enlarge them at every step.  A NaN or an infinity in a matrix makes all of it NaN, and so does a matrix of zeros with eps = 0.
  *  d_workspace: lsam_orthogonalize_workspace_bytes() bytes.
  * K <= 65535, rows, cols <= 2^20, steps 0 .. 32, eps >= 0, scale 0 or |scale| >= 2^-90, |a| >= 1 (small singular values have to grow); coefficients for which no bound of the singular values below
  * 2^10 holds throughout are refused. */

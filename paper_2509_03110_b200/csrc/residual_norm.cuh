@@ -5,8 +5,11 @@
 // Gradient, from dy and du (h = y r, dh = du w_pre):
 //   g = dy + r (dh - h m1), m1 = mean(dh h);   dx = alpha g;   dz = beta g p act'(z);   dc = beta g act(z) w_post;   db = q (dc - c m2), m2 = mean(dc c)
 //   dw_pre = sum over rows of du h;   dw_post = sum over rows of beta g act(z) c
-// All of it is bound by the bytes of the [rows, n] tensors: 32 x 256 x 4096 bf16 with a gate that is a tensor, 336 MB in 65 us forward (5.1 TB/s), 540 MB in 118 us
-// back (4.6 TB/s, one block of 16 warps an SM, half of the issue slots).  m2 depends on m1 through g, but linearly, so both come from three sums over a row that need
+// The floor is the bytes of the [rows, n] tensors: 32 x 256 x 4096 bf16 with a gate that is a tensor, 336 MB in 65 us forward (5.1 TB/s), 540 MB in 118 us
+// back (4.6 TB/s, one block of 16 warps an SM, half of the issue slots).  The same rows in other forms: forward out = x + branch and its norm 48 us
+// (5.6 TB/s), the norm alone 29 (4.6); back 128 and 97 us (3.1 and 2.1 TB/s), bound by the instructions of a row, in the form that tests for what is there.  Forward rows that do not fit
+// registers (fp32 past 8192 columns) run at 1.2 to 3.1 TB/s: single elements, the inputs read again for every reduction.
+// m2 depends on m1 through g, but linearly, so both come from three sums over a row that need
 // no order among themselves:  S1 = sum dh h,  S2 = sum a (dy + r dh),  S3 = sum a r h  with a = beta act(z) w_post c:  m1 = S1 / n, m2 = (S2 - m1 S3) / n.
 // (What cancels there is of the size of dc itself, whose own rounding is as large.)  The forward pass keeps two reductions: its sum of y^2 written that way
 // would lose all digits of r where x and the branch cancel.
